@@ -239,8 +239,114 @@ DPS_API dps_status dps_restore_residual(uint8_t* w_resid, const uint8_t* backup_
                                         size_t chunk_bytes, void* cuda_stream);
 
 /*
+ * ---- The operators of a decoder step between its linear layers ------------------------------------------------
+ * The paper's engine serves these from the system it is built on; here they stand beside the linear layers, so that
+ * a step runs from the QKV linear's output to the experts' rows in this library.  None of them synchronises, and none
+ * allocates.  They share the conventions above: nothing is enqueued on an error that the host sees, a bad index met
+ * on the device sets the status word (DPS_ERR_DATA) and is left out, and the results are deterministic.
+ */
+typedef enum { DPS_TYPE_FP16 = 0, DPS_TYPE_BF16 = 1, DPS_TYPE_FP32 = 2 } dps_type;
+
+/*
+ * A paged key-value cache: `blocks` blocks of page_tokens tokens each.  Element d of head h of token t of block b is
+ * k[b * block_stride + t * token_stride + h * head_stride + d] (and v alike), strides in elements, so that both
+ * [block][token][head][d] and [block][head][token][d], and views into larger tensors, are served.  head_dim: a
+ * multiple of 8 up to 256.  The strides are multiples of 8 elements and not negative, k and v 16-byte aligned.
+ * type: DPS_TYPE_FP16 or DPS_TYPE_BF16, the queries' type too.  The struct is read before a call returns.
+ * A SLOT is block * page_tokens + token, 64 bits wide.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    int64_t blocks, block_stride, token_stride, head_stride;
+    int32_t page_tokens, heads, head_dim, type;
+} dps_kv_cache;
+
+/*
+ * The block tables, positions and cache slots of one step, from the request lengths.
+ * Request b (0 <= b < B) has lengths[b] tokens in the cache and adds new_tokens[b] >= 0.  With
+ *   have = ceil(lengths[b] / page_tokens), need = ceil((lengths[b] + new_tokens[b]) / page_tokens)
+ * it takes need - have blocks from `granted` (G block ids, handed out by the host's block manager), the requests one
+ * after another, and they become entries have .. need-1 of its row of block_table (row stride table_stride, table_width
+ * entries); all other entries are left as they are.  Outputs:
+ *   lengths_out[b] = lengths[b] + new_tokens[b];  token_starts[B + 1]: the first of each request's rows in the step's flat
+ *   batch of tokens, and their number (2^31 - 1 where it is larger);  for each of these rows positions (from lengths[b] on) and slots, up to T rows:
+ *   rows behind the last token get position 0 and slot -1 (dps_qk_norm_rope leaves such rows alone), so a step may be
+ *   padded to the size its CUDA graph was captured for;  granted_used[0] = the blocks taken.
+ * A request is left out -- its length and its table row stay as they are, its rows get slot -1, the status word is set --
+ * if one of its numbers is negative, if it would pass table_width blocks or 2^31 - 1 tokens, if its rows would pass T, or if `granted`
+ * runs out before it is served.  A block id outside [0, blocks) is entered as -1 and its tokens get slot -1 (status too).
+ * lengths_out must not be lengths.  B up to 2^20.  All arrays are device memory; granted may be NULL if G == 0.
+ */
+DPS_API dps_status dps_extend_block_tables(const int32_t* lengths, const int32_t* new_tokens, int64_t B, const int32_t* granted,
+                                           int64_t G, int32_t* block_table, int64_t table_stride, int64_t table_width,
+                                           int32_t page_tokens, int64_t blocks, int32_t* lengths_out, int32_t* token_starts,
+                                           int32_t* positions, int64_t* slots, int64_t T, int32_t* granted_used,
+                                           void* cuda_stream);
+
+/*
+ * Norms of queries and keys for each head, position rotation and the write into the cache, in one pass over the QKV
+ * linear's output.  qkv: [T] rows of q_heads query heads, then cache->heads key heads, then as many value heads, head_dim
+ * elements each (row stride qkv_stride elements).  For each query and key head x of row t:
+ *   x <- x / sqrt(mean(x^2) + eps) * weight        (q_weight, k_weight: head_dim elements; both NULL: no norm)
+ *   the first `rotated` elements in pairs (a, b) <- (a cos - b sin, b cos + a sin) with row positions[t] of cos_sin,
+ *   float [max_position][rotated]: rotated/2 cosines, then as many sines.  Pair i is (i, i + rotated/2), or, with
+ *   interleaved != 0, (2i, 2i + 1).  rotated: a multiple of 16 up to head_dim; 0: no rotation (positions, cos_sin unused).
+ * in 32 bits with one rounding at the end.  Queries go to q_out [T][q_heads][head_dim] (row stride q_out_stride; it may
+ * be qkv itself), keys and values (unchanged) to slots[t] of the cache.  A row with a negative slot is padding: nothing of
+ * it is read or written.  A row whose slot or position is out of range is skipped and flagged.  The slots of a call must
+ * differ.  A cache of page_tokens = 1 and slots 0, 1, .. makes plain rows of keys and values.
+ */
+DPS_API dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t T, int32_t q_heads, const dps_kv_cache* cache,
+                                    const int64_t* slots, const int32_t* positions, const float* cos_sin, int64_t max_position,
+                                    int32_t rotated, int32_t interleaved, const void* q_weight, const void* k_weight, float eps,
+                                    void* q_out, int64_t q_out_stride, void* cuda_stream);
+
+/*
+ * Attention of one new token per request over the paged cache:
+ *   out[b][h][:] = sum_t p_t V[t][h / (q_heads / heads)][:],  p = softmax_t(scale * q[b][h] . K[t][h / (q_heads / heads)]),
+ * t over the lengths[b] tokens that row b of block_table names (block_table[b][t / page_tokens]).  q: [B] rows of q_heads heads
+ * (strides q_row_stride, q_head_stride, multiples of 8 elements); out: contiguous [B][q_heads][head_dim].  q_heads is
+ * a multiple of cache->heads.  Scores, softmax and sums in 32 bits, one rounding at the end.  Only tokens below the length are read, whatever stands
+ * behind them.  lengths[b] == 0 gives zeros.  A length that is negative counts as 0, one beyond table_width * page_tokens as that (status
+ * word set); the tokens of a block id outside [0, blocks) count for nothing (status word set; a row that has no other gives NaN).
+ *
+ * The cache's length is split over the GPU, and the parts are joined in a fixed order within the same launch, which takes scratch:
+ * workspace, 16-byte aligned, dps_paged_attention_workspace_bytes(q_heads, heads, head_dim) bytes (any batch and length;
+ * the largest over several layers' shapes serves them all).  Before its first use, and after anything else has written to it,
+ * it is prepared by dps_paged_attention_workspace_init; each call leaves it ready for the next.  A call that finds it
+ * unprepared computes nothing: dps_stream_status() reports DPS_ERR_WORKSPACE.  Calls that share a workspace must be
+ * ordered on the GPU (one stream, or events): two that overlap, replayed graphs among them, would take each other's parts.
+ */
+DPS_API dps_status dps_paged_attention(const void* q, int64_t q_row_stride, int64_t q_head_stride, int64_t B, int32_t q_heads,
+                                       const dps_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                                       int64_t table_width, const int32_t* lengths, float scale, void* out, void* workspace,
+                                       size_t workspace_bytes, void* cuda_stream);
+/* 0 if an argument is invalid. */
+DPS_API size_t dps_paged_attention_workspace_bytes(int32_t q_heads, int32_t kv_heads, int32_t head_dim);
+DPS_API dps_status dps_paged_attention_workspace_init(void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Routing: the experts of each token and their weights, in the form that dps_moe_linear takes.
+ * logits: [T][E] of `type` (row stride logits_stride elements).  For each row
+ *   s = softmax(logits) over all experts, or sigmoid(logits);  c = s + bias (bias: float [E], or NULL for none)
+ *   groups > 1: the E experts are `groups` groups of E / groups neighbours; a group is worth the sum of its two largest c, and
+ *   only experts of the top_groups groups worth most stay;  the top_k experts with the largest c are taken, largest first.
+ *   weight = s, divided by the sum of the taken s if renormalise != 0 (zero where that sum is zero), times scale.
+ * A choice between equal values falls on the lower index.  It is made as in 64 bits; the weights are 32 bits wide.
+ * Row t * top_k + j of the outputs is choice j of token t: expert_of_row int32, weights float, token_of_row int32 (may be NULL: it is t).
+ * A row with a NaN score or choice (a NaN logit; for softmax +Inf, or all -Inf) gets experts -1 and weights 0, and the status word is set.
+ * E up to 1024, top_k up to 32 and at most top_groups * (E / groups); groups up to 32.  groups == 1 and top_groups == 1: no groups.
+ */
+typedef enum { DPS_SCORE_SOFTMAX = 0, DPS_SCORE_SIGMOID = 1 } dps_score;
+DPS_API dps_status dps_route_experts(const void* logits, int64_t logits_stride, int32_t type, int64_t T, int32_t E, const float* bias,
+                                     int32_t scoring, int32_t groups, int32_t top_groups, int32_t top_k, int32_t renormalise,
+                                     float scale, int32_t* token_of_row, int32_t* expert_of_row, float* weights, void* cuda_stream);
+
+/*
  * Synchronises the stream, then returns and clears the current device's status word:
- * DPS_OK, DPS_ERR_DATA (a kernel skipped a row with a bad index) or DPS_ERR_CUDA.
+ * DPS_OK, DPS_ERR_DATA (a kernel skipped a row with a bad index), DPS_ERR_WORKSPACE (an attention call met a workspace that
+ * was not prepared) or DPS_ERR_CUDA.
  */
 DPS_API dps_status dps_stream_status(void* cuda_stream);
 

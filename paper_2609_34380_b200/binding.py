@@ -6,6 +6,7 @@ no CPU or PyTorch fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import hashlib
 import importlib.util
@@ -23,7 +24,18 @@ DPS_OK = 0
 DPS_ERR_NULL, DPS_ERR_SHAPE, DPS_ERR_MODE, DPS_ERR_ENCODING, DPS_ERR_ALIGN = 1, 2, 3, 4, 5
 DPS_ERR_UNSUPPORTED, DPS_ERR_CUDA, DPS_ERR_DATA, DPS_ERR_WORKSPACE = 6, 7, 8, 9
 
+DPS_TYPE_FP16, DPS_TYPE_BF16, DPS_TYPE_FP32 = 0, 1, 2
+DPS_SCORE_SOFTMAX, DPS_SCORE_SIGMOID = 0, 1
+
 LIB_PATH = Path(__file__).resolve().parent / "libdps.so"
+
+
+class KvCache(ctypes.Structure):
+    """dps_kv_cache of include/dps.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("blocks", ctypes.c_int64), ("block_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("page_tokens", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("type", ctypes.c_int32)]
+
 
 # name -> (restype, argtypes); must list every function include/dps.h declares
 _vp, _i64, _i32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
@@ -40,6 +52,14 @@ ABI = {
     "dps_linear_fp8act": (ctypes.c_int, [_i32, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp]),
     "dps_backup_residual": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t, ctypes.c_size_t, _vp]),
     "dps_restore_residual": (ctypes.c_int, [_vp, _vp, ctypes.c_size_t, ctypes.c_size_t, _vp]),
+    "dps_extend_block_tables": (ctypes.c_int, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i64, _vp, _vp, _vp, _vp, _i64, _vp, _vp]),
+    "dps_qk_norm_rope": (ctypes.c_int, [_vp, _i64, _i64, _i32, ctypes.POINTER(KvCache), _vp, _vp, _vp, _i64, _i32, _i32, _vp, _vp,
+                                        ctypes.c_float, _vp, _i64, _vp]),
+    "dps_paged_attention": (ctypes.c_int, [_vp, _i64, _i64, _i64, _i32, ctypes.POINTER(KvCache), _vp, _i64, _i64, _vp, ctypes.c_float, _vp,
+                                           _vp, ctypes.c_size_t, _vp]),
+    "dps_paged_attention_workspace_bytes": (ctypes.c_size_t, [_i32, _i32, _i32]),
+    "dps_paged_attention_workspace_init": (ctypes.c_int, [_vp, ctypes.c_size_t, _vp]),
+    "dps_route_experts": (ctypes.c_int, [_vp, _i64, _i32, _i64, _i32, _vp, _i32, _i32, _i32, _i32, _i32, ctypes.c_float, _vp, _vp, _vp, _vp]),
     "dps_stream_status": (ctypes.c_int, [_vp]),
     "dps_debug_wait_timeout": (ctypes.c_int, [ctypes.c_uint64, _vp]),
     "dps_launch_count": (_i64, []),
@@ -65,7 +85,8 @@ def fastcall_path() -> Path:
 FASTCALL_PATH = fastcall_path()
 
 # native marshalling (csrc/fastcall.cpp), set when the library is loaded, if it was built: dps_linear's, and the module with the others'
-_FASTCALL_ENTRIES = ("set_linear", "set_functions", "linear", "split_weights", "reconstruct", "moe_linear")
+_FASTCALL_ENTRIES = ("set_linear", "set_functions", "linear", "split_weights", "reconstruct", "moe_linear",
+                     "set_step_functions", "extend_block_tables", "qk_norm_rope", "paged_attention", "route_experts")
 _fast_linear = None
 _native = None
 
@@ -111,6 +132,8 @@ def _load_fastcall(lib: ctypes.CDLL) -> None:
     module.set_linear(ctypes.cast(lib.dps_linear, ctypes.c_void_p).value)
     module.set_functions(*(ctypes.cast(fn, ctypes.c_void_p).value
                            for fn in (lib.dps_split_weights, lib.dps_reconstruct, lib.dps_moe_linear)))
+    module.set_step_functions(*(ctypes.cast(fn, ctypes.c_void_p).value for fn in (
+        lib.dps_extend_block_tables, lib.dps_qk_norm_rope, lib.dps_paged_attention, lib.dps_route_experts)))
     _fast_linear, _native = module.linear, module
 
 
@@ -329,6 +352,235 @@ def dps_restore_residual(w_resid: torch.Tensor, backup_host: torch.Tensor, chunk
     st = library().dps_restore_residual(_dev(w_resid, torch.uint8, "w_resid"), _host_bytes(backup_host, "backup_host"),
                                         w_resid.numel(), int(chunk_bytes), _stream(stream))
     _check(st, "dps_restore_residual")
+
+
+# ---- the operators of a decoder step between its linear layers ----------------------------------------------------------------------
+_TYPES = {torch.float16: DPS_TYPE_FP16, torch.bfloat16: DPS_TYPE_BF16, torch.float32: DPS_TYPE_FP32}
+
+
+def _here(t: torch.Tensor, what: str) -> None:
+    """The library launches on the current device: a tensor of another one would be read across, or not at all."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _int32(value, what: str) -> int:
+    value = int(value)
+    if not -2 ** 31 <= value < 2 ** 31:     # ctypes would cut it off
+        raise ValueError(f"{what} does not fit 32 bits: {value}")
+    return value
+
+
+def _allocating_on(stream):
+    """What a call makes for itself belongs to the stream it runs on: its memory is not handed out again while that stream may use it."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream)))
+
+
+def _flat(t: Optional[torch.Tensor], dtype, what: str, count: Optional[int] = None) -> Optional[int]:
+    """Address of a contiguous tensor of this type on the current device (with this many elements)."""
+    if t is None:
+        return None
+    _here(t, what)
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{what} must have {count} elements, got {t.numel()}")
+    return _dev(t, dtype, what)
+
+
+def _rows(t: torch.Tensor, dims: int, what: str) -> int:
+    """Address of a tensor of `dims` dimensions on the current device whose last dimension is dense; the others may be strided."""
+    _here(t, what)
+    if t.dim() != dims:
+        raise ValueError(f"{what} must have {dims} dimensions, got {t.dim()}")
+    if t.numel() > 0 and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    return t.data_ptr()
+
+
+def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor) -> KvCache:
+    k, v = _rows(k_cache, 4, "k_cache"), _rows(v_cache, 4, "v_cache")
+    if k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+        raise ValueError("k_cache and v_cache must have the same shape, strides and type")
+    if k_cache.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"the cache must be float16 or bfloat16, got {k_cache.dtype}")
+    blocks, page, heads, dim = k_cache.shape
+    return KvCache(k, v, blocks, *k_cache.stride()[:3], page, heads, dim, _TYPES[k_cache.dtype])
+
+
+def dps_extend_block_tables(lengths: torch.Tensor, new_tokens: torch.Tensor, granted: Optional[torch.Tensor], block_table: torch.Tensor,
+                            page_tokens: int, blocks: int, lengths_out: Optional[torch.Tensor] = None,
+                            token_starts: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                            slots: Optional[torch.Tensor] = None, granted_used: Optional[torch.Tensor] = None, tokens: Optional[int] = None,
+                            stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Block tables of a step, in place, and (lengths_out [B], token_starts [B + 1], positions [T], slots [T], granted_used [1]).
+    T is the size of positions and slots, or `tokens` where they are to be made."""
+    if stream is None and _native is not None and granted_used is not None:
+        out = _native.extend_block_tables(lengths, new_tokens, granted, block_table, page_tokens, blocks, lengths_out, token_starts, positions,
+                                          slots, granted_used)
+        if out.__class__ is int:
+            _check(out, "dps_extend_block_tables")
+            return lengths_out, token_starts, positions, slots, granted_used
+    B = lengths.numel()
+    table = _rows(block_table, 2, "block_table")
+    if block_table.dtype != torch.int32:
+        raise TypeError(f"block_table must be torch.int32, got {block_table.dtype}")
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table must have {B} rows, got {block_table.shape[0]}")
+    made = positions if positions is not None else slots
+    T = tokens if made is None else made.numel()
+    if T is None or (tokens is not None and tokens != T):
+        raise ValueError("tokens must be given where positions and slots are not, and be their size where they are")
+    new = lambda n, dtype: torch.empty((n,), dtype=dtype, device=lengths.device)  # noqa: E731
+    with _allocating_on(stream):
+        lengths_out = new(B, torch.int32) if lengths_out is None else lengths_out
+        token_starts = new(B + 1, torch.int32) if token_starts is None else token_starts
+        positions = new(T, torch.int32) if positions is None else positions
+        slots = new(T, torch.int64) if slots is None else slots
+        granted_used = new(1, torch.int32) if granted_used is None else granted_used
+    st = library().dps_extend_block_tables(
+        _flat(lengths, torch.int32, "lengths"), _flat(new_tokens, torch.int32, "new_tokens", B), B, _flat(granted, torch.int32, "granted"),
+        0 if granted is None else granted.numel(), table, block_table.stride(0), block_table.shape[1], _int32(page_tokens, "page_tokens"), int(blocks),
+        _flat(lengths_out, torch.int32, "lengths_out", B), _flat(token_starts, torch.int32, "token_starts", B + 1),
+        _flat(positions, torch.int32, "positions", T), _flat(slots, torch.int64, "slots", T), T,
+        _flat(granted_used, torch.int32, "granted_used", 1), _stream(stream))
+    _check(st, "dps_extend_block_tables")
+    return lengths_out, token_starts, positions, slots, granted_used
+
+
+def dps_qk_norm_rope(qkv: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, slots: torch.Tensor,
+                     positions: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None,
+                     q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     interleaved: bool = False, q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Queries and keys of qkv[T][(q_heads + 2 kv_heads) * head_dim] normalised and rotated, keys and values written to slots[T] of the
+    caches [blocks][page_tokens][kv_heads][head_dim]; returns the queries [T][q_heads][head_dim]."""
+    if stream is None and _native is not None:
+        out = _native.qk_norm_rope(qkv, k_cache, v_cache, slots, positions, cos_sin, q_weight, k_weight, eps, interleaved, q_out)
+        if out.__class__ is int:
+            _check(out, "dps_qk_norm_rope")
+        if out is not None:
+            return out
+    cache = _cache(k_cache, v_cache)
+    x = _rows(qkv, 2, "qkv")
+    if qkv.dtype != k_cache.dtype:
+        raise TypeError(f"qkv must have the cache's type {k_cache.dtype}, got {qkv.dtype}")
+    T, width = qkv.shape
+    q_width = width - 2 * cache.heads * cache.head_dim
+    if q_width < 0 or q_width % cache.head_dim:
+        raise ValueError(f"qkv's rows of {width} elements are not heads of {cache.head_dim} with {cache.heads} key and value heads")
+    q_heads = q_width // cache.head_dim
+    rotated = max_position = 0
+    if cos_sin is not None:
+        if cos_sin.dim() != 2:
+            raise ValueError("cos_sin must be [positions][rotated elements]")
+        max_position, rotated = cos_sin.shape
+    if q_out is None:
+        with _allocating_on(stream):
+            q_out = torch.empty((T, q_heads, cache.head_dim), dtype=qkv.dtype, device=qkv.device)
+    out = _rows(q_out, 3, "q_out")
+    if tuple(q_out.shape) != (T, q_heads, cache.head_dim) or q_out.dtype != qkv.dtype:
+        raise ValueError(f"q_out must be {qkv.dtype} {(T, q_heads, cache.head_dim)}")
+    if q_heads > 1 and q_out.stride(1) != cache.head_dim:
+        raise ValueError("q_out: the heads of a row must be contiguous")
+    st = library().dps_qk_norm_rope(
+        x, qkv.stride(0), T, q_heads, ctypes.byref(cache), _flat(slots, torch.int64, "slots", T),
+        _flat(positions, torch.int32, "positions", T), _flat(cos_sin, torch.float32, "cos_sin"), max_position, rotated, int(bool(interleaved)),
+        _flat(q_weight, qkv.dtype, "q_weight", cache.head_dim), _flat(k_weight, qkv.dtype, "k_weight", cache.head_dim), float(eps), out,
+        q_out.stride(0), _stream(stream))
+    _check(st, "dps_qk_norm_rope")
+    return q_out
+
+
+def dps_paged_attention_workspace_bytes(q_heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(library().dps_paged_attention_workspace_bytes(int(q_heads), int(kv_heads), int(head_dim)))
+
+
+def dps_paged_attention_workspace_init(workspace: torch.Tensor, stream=None) -> torch.Tensor:
+    """Makes a uint8 tensor ready for dps_paged_attention (once; each call leaves it ready)."""
+    st = library().dps_paged_attention_workspace_init(_flat(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream))
+    _check(st, "dps_paged_attention_workspace_init")
+    return workspace
+
+
+def dps_paged_attention_workspace(q_heads: int, kv_heads: int, head_dim: int, stream=None) -> torch.Tensor:
+    """A workspace for dps_paged_attention on the current device, ready for use."""
+    need = dps_paged_attention_workspace_bytes(q_heads, kv_heads, head_dim)
+    if need == 0:
+        raise DpsError(DPS_ERR_SHAPE, "dps_paged_attention_workspace")
+    with _allocating_on(stream):
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return dps_paged_attention_workspace_init(workspace, stream)
+
+
+def dps_paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor,
+                        scale: Optional[float] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """One new token per request, q [B][q_heads][head_dim], over the caches [blocks][page_tokens][kv_heads][head_dim]; scale: 1 / sqrt(head_dim).
+    A loop keeps a workspace (dps_paged_attention_workspace); without one each call makes its own."""
+    if stream is None and _native is not None and workspace is not None:
+        res = _native.paged_attention(q, k_cache, v_cache, block_table, lengths, scale, out, workspace)
+        if res.__class__ is int:
+            _check(res, "dps_paged_attention")
+        if res is not None:
+            return res
+    cache = _cache(k_cache, v_cache)
+    x = _rows(q, 3, "q")
+    if q.dtype != k_cache.dtype:
+        raise TypeError(f"q must have the cache's type {k_cache.dtype}, got {q.dtype}")
+    B, q_heads, dim = q.shape
+    if dim != cache.head_dim:
+        raise ValueError(f"head_dim mismatch: q has {dim}, the cache {cache.head_dim}")
+    table = _rows(block_table, 2, "block_table")
+    if block_table.dtype != torch.int32:
+        raise TypeError(f"block_table must be torch.int32, got {block_table.dtype}")
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table must have {B} rows, got {block_table.shape[0]}")
+    if out is None:
+        with _allocating_on(stream):
+            out = torch.empty((B, q_heads, dim), dtype=q.dtype, device=q.device)
+    if tuple(out.shape) != (B, q_heads, dim):
+        raise ValueError(f"out must be {(B, q_heads, dim)}")
+    if workspace is None and B > 0 and q_heads % cache.heads == 0:
+        workspace = dps_paged_attention_workspace(q_heads, cache.heads, dim, stream)
+    st = library().dps_paged_attention(
+        x, q.stride(0), q.stride(1), B, q_heads, ctypes.byref(cache), table, block_table.stride(0), block_table.shape[1],
+        _flat(lengths, torch.int32, "lengths", B), dim ** -0.5 if scale is None else float(scale), _flat(out, q.dtype, "out"),
+        _flat(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _stream(stream))
+    _check(st, "dps_paged_attention")
+    return out
+
+
+def dps_route_experts(logits: torch.Tensor, top_k: int, bias: Optional[torch.Tensor] = None, scoring: int = DPS_SCORE_SOFTMAX, groups: int = 1,
+                      top_groups: int = 1, renormalise: bool = True, scale: float = 1.0, token_of_row: Optional[torch.Tensor] = None,
+                      expert_of_row: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                      stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """logits [T][E] -> (token_of_row [T * top_k], expert_of_row [T * top_k], weights [T][top_k]); the first two are what dps_moe_linear takes."""
+    if stream is None and _native is not None:
+        out = _native.route_experts(logits, top_k, bias, scoring, groups, top_groups, renormalise, scale, token_of_row, expert_of_row, weights)
+        if out.__class__ is int:
+            _check(out, "dps_route_experts")
+        if out is not None:
+            return out
+    x = _rows(logits, 2, "logits")
+    if logits.dtype not in _TYPES:
+        raise TypeError(f"logits must be float16, bfloat16 or float32, got {logits.dtype}")
+    T, E = logits.shape
+    top_k = _int32(top_k, "top_k")
+    rows = max(T * top_k, 0)
+    new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
+    with _allocating_on(stream):
+        token_of_row = new((rows,), torch.int32) if token_of_row is None else token_of_row
+        expert_of_row = new((rows,), torch.int32) if expert_of_row is None else expert_of_row
+        weights = new((T, max(top_k, 0)), torch.float32) if weights is None else weights
+    st = library().dps_route_experts(
+        x, logits.stride(0), _TYPES[logits.dtype], T, E, _flat(bias, torch.float32, "bias", E), _int32(scoring, "scoring"),
+        _int32(groups, "groups"), _int32(top_groups, "top_groups"), top_k,
+        int(bool(renormalise)), float(scale), _flat(token_of_row, torch.int32, "token_of_row", rows),
+        _flat(expert_of_row, torch.int32, "expert_of_row", rows), _flat(weights, torch.float32, "weights", rows), _stream(stream))
+    _check(st, "dps_route_experts")
+    return token_of_row, expert_of_row, weights
 
 
 def dps_stream_status(stream=None) -> int:

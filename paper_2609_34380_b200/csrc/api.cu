@@ -369,7 +369,7 @@ dps_status dps_stream_status(void* cuda_stream) {
         return DPS_ERR_CUDA;
     if (cudaMemsetAsync(d->status, 0, sizeof(int), stream) != cudaSuccess) return DPS_ERR_CUDA;
     if (cudaStreamSynchronize(stream) != cudaSuccess) return DPS_ERR_CUDA;
-    return word == 0 ? DPS_OK : (word == (int)DPS_ERR_DATA ? DPS_ERR_DATA : DPS_ERR_CUDA);
+    return word == DPS_OK || word == DPS_ERR_DATA || word == DPS_ERR_WORKSPACE ? (dps_status)word : DPS_ERR_CUDA;
 }
 
 dps_status dps_quantize_activations(const void* x, uint8_t* x_fp8, float* scale, int64_t M, int64_t K,
