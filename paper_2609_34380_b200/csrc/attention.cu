@@ -7,8 +7,9 @@
 //   * The work is a flat list of tiles, 64 tokens of one (request, key-value head) each, in that order.  A resident grid cuts it into
 //     equal runs, one per CTA, whatever the lengths are: each CTA sums the lengths itself (they are on the device) and finds its
 //     run's start.  So one long request is spread over the GPU, and a ragged batch leaves no SM behind.
-//   * A warp owns 16 tokens of each tile and a ring of asynchronous 16-byte copies of its own: no barrier inside a run, and the
-//     copies run on across the borders of requests and heads.  The ids of the blocks are fetched one tile ahead of the copies.
+//   * Warps that copy feed warps that compute, each of the latter with 16 tokens of every tile and a ring of stages of its own: no
+//     barrier among them inside a run, and the copies run on across the borders of requests and heads.  The tokens' blocks are looked
+//     up one tile ahead, so a page may end anywhere.
 //   * Keys times queries: S^T (16 tokens x 8 heads) = K (16 x dim) Q^T by m16n8k16 products, the tokens being the rows of the
 //     matrix product: up to eight heads that share the keys cost one column block, one head alone does too.  The scores' maximum and sum run along (in 32
 //     bits, by powers of two).  Values: O^T (dim x 8 heads) += V^T P^T, where P is handed over as the sum of two 16-bit values, so
@@ -26,8 +27,8 @@ namespace {
 
 using warp::Half2;
 
-constexpr int kThreads = 128;
-constexpr int kWarps = 4;
+constexpr int kWarps = 4;             // that compute; further ones copy
+constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 64;             // tokens of a tile
 constexpr int kWarpTokens = 16;       // ... of them a warp's
 constexpr int kMaxCtas = 1024;        // counters in the workspace
@@ -50,6 +51,7 @@ struct AttentionParams {
     int* status;
     int64_t longest;      // tokens that a row of the table can name
     int page, kv_heads, dim, group, chunks, requests;
+    unsigned page_magic, page_shift;      // token / page = token * page_magic >> page_shift, for tokens below 2^31
     float scale_log2;
 };
 
@@ -58,6 +60,8 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Orders this thread's view of memory, shared and global, in front of the bulk copies that it issues next.
+__device__ __forceinline__ void fence_proxies() { asm volatile("fence.proxy.async;" ::: "memory"); }
 __device__ __forceinline__ int clamped_length(const AttentionParams& p, int b) {
     const int n = p.lengths[b];
     return n <= 0 ? 0 : (int64_t)n > p.longest ? (int)p.longest : n;
@@ -67,8 +71,7 @@ __device__ __forceinline__ int tiles_of(int length) { return (int)(((unsigned)le
 // A place in the list of tiles.
 struct Place {
     int b, h, j, tiles, length;    // request, key-value head (and chunk of its queries), tile of them; the request's tiles and tokens
-    __device__ __forceinline__ void next(const AttentionParams& p, int heads) {
-        if (++j < tiles) return;
+    __device__ __forceinline__ void next_unit(const AttentionParams& p, int heads) {
         j = 0;
         if (++h < heads) return;
         h = 0;
@@ -76,16 +79,24 @@ struct Place {
         while (length == 0 && b + 1 < p.requests);
         tiles = tiles_of(length);
     }
+    __device__ __forceinline__ void next(const AttentionParams& p, int heads) {
+        if (++j == tiles) next_unit(p, heads);
+    }
 };
 
 template <int DP, int NB>
 struct Shape {
-    static constexpr int kStageBytes = kWarpTokens * DP * 2 * 2;            // a warp's keys and values
+    static constexpr int kRowBytes = DP * 2;
+    static constexpr int kValues = kWarpTokens * kRowBytes;                 // where the values start in a stage
+    static constexpr int kStageBytes = 2 * kValues;
     static constexpr int kStages = DP == 64 ? 6 : 3;
     static constexpr int kCtas = DP == 256 ? 1 : 2;                         // per SM
-    static constexpr int kPitch = DP + 4;                                   // floats of a head's row while warps are joined
-    static constexpr int kJoinBytes = kWarps * 8 * kPitch * 4;
-    static constexpr int kBytes = kWarps * kStages * kStageBytes + kJoinBytes;
+    // warps that copy: as many as leave the others the registers they need
+    static constexpr int kProducers = DP == 256 ? 4 : 2;
+    static constexpr bool kQueriesAhead = NB * DP < 256;                    // the next queries wait in registers
+    static constexpr int kAllThreads = kThreads + 32 * kProducers;
+    static_assert(8 * DP * 4 <= kValues, "a warp's sums take the place of the values it has read last");
+    static constexpr int kBytes = kWarps * kStages * kStageBytes;
     static constexpr int kPartFloats = 8 * NB * (DP + 2);                   // a part: sums, then maximum and total of each head
 };
 
@@ -115,30 +126,45 @@ struct Joined {
     }
 };
 
+// A (request, head) that several CTAs hold parts of: the CTAs.
+struct Split {
+    int first = 0, last = -1;      // none
+    int b = 0, h = 0;
+};
+
 template <typename T, int DP, int NB>
-__global__ void __launch_bounds__(kThreads, (Shape<DP, NB>::kCtas))
+__global__ void __launch_bounds__((Shape<DP, NB>::kAllThreads), (Shape<DP, NB>::kCtas))
 paged_attention_kernel(const AttentionParams p) {
     using S = Shape<DP, NB>;
-    constexpr int kRowChunks = DP / 8;                                      // 16-byte chunks of a token's keys
-    constexpr int kCopies = kWarpTokens * kRowChunks / 32;
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ __align__(1024) unsigned char smem[];                 // the rows are aligned to their size
+    __shared__ __align__(8) uint64_t s_full[kWarps][S::kStages], s_empty[kWarps][S::kStages], s_join;
     __shared__ int64_t s_scan[kWarps];
     __shared__ unsigned s_mask[kWarps][S::kStages];
-    __shared__ float2 s_stat[kWarps][8];
+    __shared__ float2 s_stat[kWarps][8], s_total[8 * NB];
+    __shared__ float s_weight[8 * NB][32];
     __shared__ Place s_first;
-    __shared__ int s_flag;
+    __shared__ int s_flag[2];
 
     sm100::grid_launch_dependents();
+    const int tid = threadIdx.x, lane = tid & 31, warp_id = tid >> 5;
+    if (lane == 0 && warp_id < kWarps) {
+        for (int i = 0; i < S::kStages; ++i) {
+            sm100::mbar_init(sm100::smem_u32(&s_full[warp_id][i]), 33);     // 32 lanes' copies and the mask
+            sm100::mbar_init(sm100::smem_u32(&s_empty[warp_id][i]), 1);
+        }
+        if (warp_id == 0) sm100::mbar_init(sm100::smem_u32(&s_join), 1);
+        sm100::fence_barrier_init();
+    }
+    __syncwarp();
     sm100::grid_dependency_wait();
 
-    const int tid = threadIdx.x, lane = tid & 31, warp_id = tid >> 5;
     const int heads = p.kv_heads * p.chunks;
     const int ctas = gridDim.x, cta = blockIdx.x;
 
     // ---- the list's length, and where this CTA's run starts
-    if (tid == 0) s_flag = *reinterpret_cast<const uint64_t*>(p.workspace) == kReady;
+    if (tid == 0) s_flag[0] = *reinterpret_cast<const uint64_t*>(p.workspace) == kReady;
     const int per = (p.requests + kThreads - 1) / kThreads;
-    const int first_request = min(tid * per, p.requests), last_request = min(first_request + per, p.requests);
+    const int first_request = min(tid * per, p.requests), last_request = warp_id < kWarps ? min(first_request + per, p.requests) : first_request;
     int64_t mine = 0;
     for (int b = first_request; b < last_request; ++b) mine += tiles_of(clamped_length(p, b));
     int64_t upto = mine;
@@ -146,9 +172,9 @@ paged_attention_kernel(const AttentionParams p) {
         const int64_t u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
         if (lane >= o) upto += u;
     }
-    if (lane == 31) s_scan[warp_id] = upto;
+    if (lane == 31 && warp_id < kWarps) s_scan[warp_id] = upto;
     __syncthreads();
-    if (!s_flag) {                                                          // a workspace that was not prepared
+    if (!s_flag[0]) {                                                       // a workspace that was not prepared
         if (cta == 0 && tid == 0) atomicExch(p.status, (int)DPS_ERR_WORKSPACE);
         return;
     }
@@ -157,12 +183,14 @@ paged_attention_kernel(const AttentionParams p) {
         if (w < warp_id) before += s_scan[w];
         total += s_scan[w];
     }
-    const int64_t all = total * heads, each = all / ctas;
+    const int64_t all = total * heads;
+    const bool narrow = all <= INT32_MAX;                                   // (64-bit divisions take 100 ns each)
+    const int64_t each = narrow ? (int)all / ctas : all / ctas;
     const int more = (int)(all - each * ctas);                              // the first CTAs have one tile more
     const int64_t start = cta * each + min(cta, more);
-    const int64_t count = each + (cta < more ? 1 : 0);
+    const int count = (int)each + (cta < more ? 1 : 0);                     // (below 2^31: checked on the host)
     if (count > 0) {
-        const int64_t at = start / heads;                                   // in tiles of requests
+        const int64_t at = narrow ? (int)start / heads : start / heads;     // in tiles of requests
         if (at >= before && at < before + mine) {
             int b = first_request;
             int64_t from = before;
@@ -173,109 +201,200 @@ paged_attention_kernel(const AttentionParams p) {
                 tiles = tiles_of(length);
             }
             const int64_t inside = start - from * heads;
-            const int h = (int)(inside / tiles);
+            const int h = narrow ? (int)inside / tiles : (int)(inside / tiles);
             s_first = Place{b, h, (int)(inside - (int64_t)h * tiles), tiles, length};
         }
     }
     // requests without tokens: zeros; a length that is none
-    for (int b = cta; b < p.requests; b += ctas) {
-        const int n = p.lengths[b];
-        if (tid == 0 && (n < 0 || (int64_t)n > p.longest)) atomicExch(p.status, (int)DPS_ERR_DATA);
-        if (n <= 0 || p.longest == 0) {
-            const int64_t row = (int64_t)p.kv_heads * p.group * p.dim / 8;
-            uint4* to = reinterpret_cast<uint4*>(p.out) + b * row;
-            for (int64_t i = tid; i < row; i += kThreads) to[i] = make_uint4(0, 0, 0, 0);
+    const auto look_for_empty = [&] {
+        for (int b = cta; b < p.requests; b += ctas) {
+            const int n = p.lengths[b];
+            if (tid == 0 && (n < 0 || (int64_t)n > p.longest)) atomicExch(p.status, (int)DPS_ERR_DATA);
+            if (n <= 0 || p.longest == 0) {
+                const int64_t row = (int64_t)p.kv_heads * p.group * p.dim / 8;
+                uint4* to = reinterpret_cast<uint4*>(p.out) + b * row;
+                for (int64_t i = tid; i < row; i += kThreads) to[i] = make_uint4(0, 0, 0, 0);
+            }
         }
+    };
+    if (count == 0) {
+        if (warp_id < kWarps) look_for_empty();
+        return;
     }
-    if (count == 0) return;
     __syncthreads();
 
-    // ---- copies into the ring
-    const uint32_t ring = sm100::smem_u32(smem) + warp_id * S::kStages * S::kStageBytes;
-    const unsigned char* const k_base = static_cast<const unsigned char*>(p.k);
-    const unsigned char* const v_base = static_cast<const unsigned char*>(p.v);
-    Place ahead = s_first;
-    int64_t left = count;                                                   // tiles not yet asked for
-    auto block_of = [&](const Place& at) {                                  // of this lane's row
-        const int64_t token = (int64_t)at.j * kTile + warp_id * kWarpTokens + (lane & 15);
-        return token < at.length ? p.table[at.b * p.table_stride + (int)token / p.page] : 0;
-    };
-    int block = block_of(ahead);
-    auto ask = [&](int stage) {
-        if (left > 0) {
-            const int64_t token = (int64_t)ahead.j * kTile + warp_id * kWarpTokens + (lane & 15);
-            const bool inside = token < ahead.length, known = (unsigned)block < (uint64_t)p.blocks;
-            if (inside && !known) atomicExch(p.status, (int)DPS_ERR_DATA);
-            const unsigned mask = __ballot_sync(0xFFFFFFFFu, inside && known) & 0xFFFFu;
-            if (lane == 0) s_mask[warp_id][stage] = mask;
-            const int64_t off = inside && known ? (block * p.block_stride + ((int)token % p.page) * p.token_stride +
-                                                   (ahead.h / p.chunks) * p.head_stride) * 2 : 0;
-            if (mask != 0) {
-                const uint32_t to = ring + stage * S::kStageBytes;
+    // ---- the warps that copy: each serves kServed of the others, 16 tokens of every tile for each
+    if (warp_id >= kWarps) {
+        constexpr int kServed = kWarps / S::kProducers, kLooks = (kServed * kWarpTokens + 31) / 32;
+        constexpr int kRowChunks = DP / 8, kRowsAtOnce = 32 / kRowChunks;   // 16-byte chunks of a row, rows of one copy instruction
+        // A lane copies chunk c of rows lane_row, lane_row + kRowsAtOnce, ...  Chunk c of row t lies at t * kRowBytes + (c ^ (t & 7)) * 16, so
+        // that the eight rows of a matrix fragment fall on different banks; an exclusive or of the whole address does it, the rows being aligned.
+        const int served = (warp_id - kWarps) * kServed;                    // the first one
+        const int lane_row = lane / kRowChunks, lane_chunk = lane % kRowChunks;
+        const uint32_t lane_dst = sm100::smem_u32(smem) + served * S::kStages * S::kStageBytes + lane_row * S::kRowBytes + ((lane_chunk ^ lane_row) << 4);
+        const unsigned char* const lane_src = static_cast<const unsigned char*>(p.k) + lane_chunk * 16;
+        const int64_t to_values = static_cast<const unsigned char*>(p.v) - static_cast<const unsigned char*>(p.k);
+        const int64_t row_step = p.token_stride * 2;
+        const bool chunk_there = lane_chunk * 8 < p.dim;
+        const bool eights = p.page % 8 == 0;                                // eight rows in a row lie in one block, a token stride apart
+        Place at = s_first;
+        int id[kLooks], within[kLooks];                                     // of this lane's tokens: the block and the place in it
+        int64_t head_off = 0;
+        auto token_of = [&](int l) { return at.j * kTile + served * kWarpTokens + l * 32 + lane; };   // (a last tile's last token is below 2^31)
+        auto mine_of = [&](int l) { return token_of(l) < at.length && l * 32 + lane < kServed * kWarpTokens; };
+        auto look_up = [&](bool first) {
+            if (first || at.j == 0) head_off = (int64_t)(p.chunks == 1 ? at.h : at.h / p.chunks) * p.head_stride;
 #pragma unroll
-                for (int i = 0; i < kCopies; ++i) {
-                    const int at = i * 32 + lane, row = at / kRowChunks, c = at % kRowChunks;
-                    const int64_t from = __shfl_sync(0xFFFFFFFFu, off, row) + c * 16;
-                    const bool wanted = ((mask >> row) & 1u) && c * 8 < p.dim;
-                    const uint32_t dst = to + row * (DP * 2) + ((c ^ (row & 7)) << 4);
-                    warp::copy16(dst, k_base + (wanted ? from : 0), wanted ? 16 : 0);
-                    warp::copy16(dst + kWarpTokens * DP * 2, v_base + (wanted ? from : 0), wanted ? 16 : 0);
+            for (int l = 0; l < kLooks; ++l)
+                if (mine_of(l)) {
+                    const int index = (int)(((uint64_t)(unsigned)token_of(l) * p.page_magic) >> p.page_shift);
+                    within[l] = token_of(l) - index * p.page;
+                    id[l] = p.table[at.b * p.table_stride + index];
                 }
+        };
+        look_up(true);
+        int stage = 0;
+        uint32_t parity = 1;                                                // the first round of the ring waits for nobody
+        for (int done = 0; done < count; ++done) {
+            int64_t off[kLooks];
+            unsigned wanted[kLooks];
+#pragma unroll
+            for (int l = 0; l < kLooks; ++l) {
+                const bool inside = mine_of(l), known = inside && (unsigned)id[l] < (uint64_t)p.blocks;
+                if (inside && !known) atomicExch(p.status, (int)DPS_ERR_DATA);
+                off[l] = known ? (id[l] * p.block_stride + within[l] * p.token_stride + head_off) * 2 : 0;
+                wanted[l] = __ballot_sync(0xFFFFFFFFu, known);
             }
-            if (--left > 0) {
-                ahead.next(p, heads);
-                block = block_of(ahead);
+            if (done + 1 < count) {
+                at.next(p, heads);
+                look_up(false);
+            }
+#pragma unroll
+            for (int c = 0; c < kServed; ++c) {
+                const uint32_t full = sm100::smem_u32(&s_full[served + c][stage]);
+                if (!sm100::mbar_wait(sm100::smem_u32(&s_empty[served + c][stage]), parity)) {
+                    if (lane == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
+                    warp::copies_wait();
+                    return;
+                }
+                const int64_t c_off = off[c * kWarpTokens / 32];
+                const unsigned mask = (wanted[c * kWarpTokens / 32] >> (c * kWarpTokens % 32)) & 0xFFFFu;
+                if (mask != 0) {
+                    const uint32_t dst = lane_dst + (c * S::kStages + stage) * S::kStageBytes;
+                    const unsigned lane_mask = chunk_there ? mask >> lane_row : 0u;
+                    const unsigned char* row = lane_src;
+#pragma unroll
+                    for (int first = 0; first < kWarpTokens; first += kRowsAtOnce) {
+                        if (!eights) row = lane_src + __shfl_sync(0xFFFFFFFFu, c_off, c * kWarpTokens % 32 + first + lane_row);
+                        else if (first % 8 == 0) row = lane_src + __shfl_sync(0xFFFFFFFFu, c_off, c * kWarpTokens % 32 + first) + lane_row * row_step;
+                        else row += kRowsAtOnce * row_step;
+                        const bool there = (lane_mask >> first) & 1u;
+                        const unsigned char* from = there ? row : static_cast<const unsigned char*>(p.k);
+                        const uint32_t to = (dst ^ ((first & 7) << 4)) + first * S::kRowBytes;
+                        warp::copy16(to, from, there ? 16 : 0);
+                        warp::copy16(to + S::kValues, from + to_values, there ? 16 : 0);
+                    }
+                }
+                if (lane == 0) {
+                    s_mask[served + c][stage] = mask;
+                    sm100::mbar_arrive(full);
+                }
+                warp::copies_arrive(full);
+            }
+            if (++stage == S::kStages) {
+                stage = 0;
+                parity ^= 1;
             }
         }
-        warp::copy_commit();
-    };
-#pragma unroll
-    for (int s = 0; s < S::kStages - 1; ++s) ask(s);
+        warp::copies_wait();
+        return;
+    }
 
-    // ---- the run
-    uint32_t qf[NB][DP / 16][2];
-    float o[NB][DP / 16][4], m[NB][2], l[NB][2];
+    // ---- the warps that compute
     const int column = lane & 3, row = lane >> 2;                           // of a fragment: heads 2 column, 2 column + 1; token row
+    // queries of a (request, head): fragments of Q^T; where registers allow, the next one's are fetched while this one's tokens are read
+    uint32_t qf[NB][DP / 16][2], q_next[NB][DP / 16][2];
+    auto fetch_queries = [&](const Place& of, uint32_t (&to)[NB][DP / 16][2]) {
+        const int kv = p.chunks == 1 ? of.h : of.h / p.chunks, chunk = of.h - kv * p.chunks;
+        const unsigned char* base = static_cast<const unsigned char*>(p.q) + (of.b * p.q_row + ((int64_t)kv * p.group + chunk * 8 * NB) * p.q_head) * 2;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int head = nb * 8 + row;
+            const bool there = chunk * 8 * NB + head < p.group;
+            const unsigned char* q_row = base + (there ? head * p.q_head : 0) * 2;
+#pragma unroll
+            for (int i = 0; i < DP / 16; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int d = i * 16 + e * 8 + column * 2;
+                    to[nb][i][e] = there && d < p.dim ? *reinterpret_cast<const uint32_t*>(q_row + d * 2) : 0u;
+                }
+        }
+    };
+    float o[NB][DP / 16][4], m[NB][2], l[NB][2];
     Place at = s_first;
+    if (S::kQueriesAhead) fetch_queries(at, q_next);
+    look_for_empty();
     bool fresh = true;                                                      // a (request, head) starts here
     const bool from_start = at.j == 0;                                      // the run's first one starts with it
-    bool first_unit = true;
-    int stage = 0;
-    const uint32_t k_lane = (lane & 15) * (DP * 2);                         // ldmatrix row of the keys: tokens 0-15, chunk 0 or 1
-    const uint32_t v_row = (lane & 7) + ((lane >> 4) << 3);                 // of the values: tokens 0-7 / 8-15, chunk by bit 3
+    bool first_unit = true, lost = false;                                   // lost: a copy did not arrive in time
+    Split head_split, tail_split;                                           // of the run's first and last (request, head)
+    // ldmatrix rows: of the keys tokens 0-15 of chunk 0, then of chunk 1; of the values tokens 0-7 of chunk 0 and of 1, then 8-15
+    const uint32_t ring = sm100::smem_u32(smem) + warp_id * S::kStages * S::kStageBytes;
+    const uint32_t k_frag = ring + (lane & 15) * S::kRowBytes + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t v_frag = ring + S::kValues + ((lane & 7) + ((lane >> 4) << 3)) * S::kRowBytes + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+    unsigned* const counters = reinterpret_cast<unsigned*>(p.workspace + kHeaderBytes);
+    float* const parts = reinterpret_cast<float*>(p.workspace + kHeaderBytes + kCounterBytes);
+    constexpr int kQuads = DP / 4, kHeadsAtOnce = kThreads / kQuads;
+    const int quad = tid % kQuads, sub = tid / kQuads;
+    auto kv_of = [&](int h) { return p.chunks == 1 ? h : h / p.chunks; };
+    auto heads_of = [&](int h) { return p.chunks == 1 ? p.group : min(p.group - h % p.chunks * 8 * NB, 8 * NB); };
+    auto store = [&](int b, int h, int head, const float4& v, float factor) {
+        if (quad * 4 < p.dim) {
+            T* const out = static_cast<T*>(p.out) +
+                           (((int64_t)b * p.kv_heads + kv_of(h)) * p.group + (h - kv_of(h) * p.chunks) * 8 * NB + head) * p.dim + quad * 4;
+            uint2 packed;
+            packed.x = Half2<T>::pack(v.x * factor, v.y * factor);
+            packed.y = Half2<T>::pack(v.z * factor, v.w * factor);
+            *reinterpret_cast<uint2*>(out) = packed;
+        }
+    };
+    auto meet = [] {                                                        // of the computing warps
+        __syncwarp();
+        sm100::named_barrier_sync(1, kThreads);
+    };
 
-    for (int64_t done = 0; done < count; ++done) {
+    int stage = 0;
+    uint32_t parity = 0;
+    for (int done = 0; done < count; ++done) {
         if (fresh) {
             fresh = false;
-            const int kv = at.h / p.chunks, chunk = at.h % p.chunks;
-            const unsigned char* q_base = static_cast<const unsigned char*>(p.q) +
-                                          (at.b * p.q_row + ((int64_t)kv * p.group + chunk * 8 * NB) * p.q_head) * 2;
+            if (!S::kQueriesAhead) fetch_queries(at, qf);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                const int head = nb * 8 + row;
-                const bool there = chunk * 8 * NB + head < p.group;
-                const unsigned char* q_row = q_base + (there ? head * p.q_head : 0) * 2;
 #pragma unroll
-                for (int i = 0; i < DP / 16; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int d = i * 16 + e * 8 + column * 2;
-                        qf[nb][i][e] = there && d < p.dim ? *reinterpret_cast<const uint32_t*>(q_row + d * 2) : 0u;
+                for (int i = 0; i < DP / 16; ++i) {
+                    if (S::kQueriesAhead) {
+                        qf[nb][i][0] = q_next[nb][i][0];
+                        qf[nb][i][1] = q_next[nb][i][1];
                     }
-                m[nb][0] = m[nb][1] = -INFINITY;
-                l[nb][0] = l[nb][1] = 0.f;
-#pragma unroll
-                for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[nb][i][e] = 0.f;
+                }
+                m[nb][0] = m[nb][1] = -INFINITY;
+                l[nb][0] = l[nb][1] = 0.f;
+            }
+            if (S::kQueriesAhead && done + at.tiles - at.j < count) {
+                Place soon = at;
+                soon.next_unit(p, heads);
+                fetch_queries(soon, q_next);
             }
         }
-        warp::copy_wait<S::kStages - 2>();
+        if (!lost && !sm100::mbar_wait(sm100::smem_u32(&s_full[warp_id][stage]), parity)) lost = true;
         __syncwarp();
-        ask(stage == 0 ? S::kStages - 1 : stage - 1);                       // the stage that the step before has read
         const unsigned mask = s_mask[warp_id][stage];
         if (mask != 0) {
-            const uint32_t keys = ring + stage * S::kStageBytes, values = keys + kWarpTokens * DP * 2;
+            const uint32_t keys = k_frag + stage * S::kStageBytes, values = v_frag + stage * S::kStageBytes;
             float s[NB][2][4];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
@@ -284,7 +403,7 @@ paged_attention_kernel(const AttentionParams p) {
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
                 uint32_t a[4];
-                warp::ldmatrix_x4(a, keys + k_lane + (((i * 2 + (lane >> 4)) ^ (lane & 7)) << 4));
+                warp::ldmatrix_x4(a, keys ^ (i << 5));
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) Half2<T>::mma(s[nb][i & 1], a, qf[nb][i][0], qf[nb][i][1]);
             }
@@ -328,7 +447,7 @@ paged_attention_kernel(const AttentionParams p) {
 #pragma unroll
             for (int i = 0; i < DP / 16; ++i) {
                 uint32_t a[4];
-                warp::ldmatrix_x4_trans(a, values + v_row * (DP * 2) + (((i * 2 + ((lane >> 3) & 1)) ^ (lane & 7)) << 4));
+                warp::ldmatrix_x4_trans(a, values ^ (i << 5));
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
                     Half2<T>::mma(o[nb][i], a, ph[nb][0], ph[nb][1]);
@@ -336,38 +455,31 @@ paged_attention_kernel(const AttentionParams p) {
                 }
             }
         }
-        if (++stage == S::kStages) stage = 0;
 
         // ---- the end of a (request, head), or of the run
         const bool ends = at.j == at.tiles - 1;
         if (ends || done + 1 == count) {
             const bool starts_here = !first_unit || from_start;
             const bool whole = ends && starts_here;
-            // of the split: its first tile in the list, its first and last CTA
-            const int64_t unit = start + done - at.j, unit_last = unit + at.tiles - 1;
-            const int64_t big = (int64_t)more * (each + 1);
-            const int cta0 = (int)(unit < big ? unit / (each + 1) : more + (unit - big) / each);
-            const int cta1 = (int)(unit_last < big ? unit_last / (each + 1) : more + (unit_last - big) / each);
-            unsigned* const counters = reinterpret_cast<unsigned*>(p.workspace + kHeaderBytes);
-            float* const parts = reinterpret_cast<float*>(p.workspace + kHeaderBytes + kCounterBytes);
-            float* const part = parts + (int64_t)(2 * cta + (starts_here ? 1 : 0)) * S::kPartFloats;
-            const int kv = at.h / p.chunks, chunk = at.h % p.chunks;
-            const int used = min(p.group - chunk * 8 * NB, 8 * NB);         // heads
-            T* const out = static_cast<T*>(p.out) + ((int64_t)at.b * p.kv_heads * p.group + (int64_t)kv * p.group + chunk * 8 * NB) * p.dim;
-            constexpr int kQuads = DP / 4, kHeadsAtOnce = kThreads / kQuads;
-            const int quad = tid % kQuads, sub = tid / kQuads;
-            float* const join = reinterpret_cast<float*>(smem + kWarps * S::kStages * S::kStageBytes);
-            auto store = [&](int head, const Joined& r) {
-                if (head < used && quad * 4 < p.dim) {
-                    const float inv = 1.f / r.l;
-                    uint2 packed;
-                    packed.x = Half2<T>::pack(r.o.x * inv, r.o.y * inv);
-                    packed.y = Half2<T>::pack(r.o.z * inv, r.o.w * inv);
-                    *reinterpret_cast<uint2*>(out + (int64_t)head * p.dim + quad * 4) = packed;
-                }
+            // the stage just read is this warp's until it hands it back: its sums for the others, element d of a head at d ^ (head / 2 % 4 * 8),
+            // which spreads the fragments over the banks
+            auto sum_of = [&](int w, int head, int d) {
+                return reinterpret_cast<float*>(smem + (w * S::kStages + stage) * S::kStageBytes + S::kValues) + head * DP + (d ^ ((head >> 1 & 3) * 8));
             };
+            float* const part = parts + (int64_t)(2 * cta + (starts_here ? 1 : 0)) * S::kPartFloats;
+            if (!whole) {                                                   // its first and last tile in the list, and their CTAs
+                const int64_t unit = start + done - at.j, unit_last = unit + at.tiles - 1, big = (int64_t)more * (each + 1);
+                Split of;
+                of.first = (int)(unit < big ? unit / (each + 1) : more + (unit - big) / each);
+                of.last = (int)(unit_last < big ? unit_last / (each + 1) : more + (unit_last - big) / each);
+                of.b = at.b;
+                of.h = at.h;
+                if (starts_here) tail_split = of;
+                else head_split = of;
+            }
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
+                __syncwarp();
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
 #pragma unroll
@@ -380,57 +492,121 @@ paged_attention_kernel(const AttentionParams p) {
                 for (int i = 0; i < DP / 16; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        join[(warp_id * 8 + 2 * column + (e & 1)) * S::kPitch + i * 16 + row + (e >> 1) * 8] = o[nb][i][e];
-                __syncthreads();
+                        *sum_of(warp_id, 2 * column + (e & 1), i * 16 + row + (e >> 1) * 8) = o[nb][i][e];
+                meet();
 #pragma unroll
                 for (int head = sub; head < 8; head += kHeadsAtOnce) {
+                    if (nb * 8 + head >= heads_of(at.h)) break;
                     Joined r;
 #pragma unroll
                     for (int w = 0; w < kWarps; ++w) {
                         const float2 st = s_stat[w][head];
-                        r.add(st.x, st.y, *reinterpret_cast<const float4*>(&join[(w * 8 + head) * S::kPitch + quad * 4]));
+                        r.add(st.x, st.y, *reinterpret_cast<const float4*>(sum_of(w, head, quad * 4)));
                     }
-                    if (whole) store(nb * 8 + head, r);
+                    if (whole) store(at.b, at.h, nb * 8 + head, r.o, 1.f / r.l);
                     else {
                         *reinterpret_cast<float4*>(part + (nb * 8 + head) * DP + quad * 4) = r.o;
                         if (quad == 0) *reinterpret_cast<float2*>(part + 8 * NB * DP + (nb * 8 + head) * 2) = make_float2(r.m, r.l);
                     }
                 }
-                __syncthreads();
-            }
-            if (!whole) {
-                __threadfence();
-                __syncthreads();
-                if (tid == 0) s_flag = atomicAdd(&counters[cta0], 1u) == (unsigned)(cta1 - cta0);
-                __syncthreads();
-                if (s_flag) {                                               // all parts are there: join them
-                    __threadfence();
-                    for (int head = sub; head < used; head += kHeadsAtOnce) {
-                        Joined r;
-                        constexpr int kBatch = 8;
-                        for (int c = cta0; c <= cta1; c += kBatch) {
-                            float2 st[kBatch];
-                            float4 v[kBatch];
-#pragma unroll
-                            for (int i = 0; i < kBatch; ++i)
-                                if (c + i <= cta1) {
-                                    const float* from = parts + (int64_t)(2 * (c + i) + (c + i == cta0 ? 1 : 0)) * S::kPartFloats;
-                                    st[i] = __ldcg(reinterpret_cast<const float2*>(from + 8 * NB * DP + head * 2));
-                                    v[i] = __ldcg(reinterpret_cast<const float4*>(from + head * DP + quad * 4));
-                                }
-#pragma unroll
-                            for (int i = 0; i < kBatch; ++i)
-                                if (c + i <= cta1) r.add(st[i].x, st[i].y, v[i]);
-                        }
-                        store(head, r);
-                    }
-                    if (tid == 0) counters[cta0] = 0;
-                }
+                meet();
             }
             fresh = true;
             first_unit = false;
         }
+        __syncwarp();
+        if (lane == 0) sm100::mbar_arrive(sm100::smem_u32(&s_empty[warp_id][stage]));
+        if (++stage == S::kStages) {
+            stage = 0;
+            parity ^= 1;
+        }
         if (done + 1 < count) at.next(p, heads);
+    }
+    if (lost && lane == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
+
+    // ---- the splits that this CTA holds a part of: whoever comes last joins the parts, in their order
+    if (head_split.last < 0 && tail_split.last < 0) return;
+    __threadfence();
+    meet();
+    if (tid < 2) {
+        const Split of = tid == 0 ? head_split : tail_split;
+        s_flag[tid] = of.last >= 0 && atomicAdd(&counters[of.first], 1u) == (unsigned)(of.last - of.first);
+    }
+    meet();
+    uint32_t join_parity = 0;
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i) {
+        if (!s_flag[i]) continue;
+        __threadfence();
+        const Split of = i == 0 ? head_split : tail_split;
+        const int n = of.last - of.first + 1, used = heads_of(of.h);
+        // As many parts at a time as the ring holds (nobody else copies any more), each by one bulk copy: they are in flight together, and asking for
+        // them costs one instruction (by 16-byte copies, with all threads asking, the 37 parts of a long request took 7 us).
+        constexpr int kAtOnce = S::kBytes / (S::kPartFloats * 4) < 32 ? S::kBytes / (S::kPartFloats * 4) : 32;
+        constexpr int kMine = 8 * NB / kHeadsAtOnce;                        // heads of a thread
+        const float* const held = reinterpret_cast<const float*>(smem);
+        float4 r[kMine];
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) r[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        float top[2 * NB], sum[2 * NB];                                     // of this warp's heads, running
+#pragma unroll
+        for (int x = 0; x < 2 * NB; ++x) top[x] = -INFINITY, sum[x] = 0.f;
+        for (int c0 = 0; c0 < n; c0 += kAtOnce) {
+            const int now = min(kAtOnce, n - c0);
+            if (warp_id == 0) {
+                if (lane == 0) sm100::mbar_arrive_expect_tx(sm100::smem_u32(&s_join), now * S::kPartFloats * 4);
+                __syncwarp();
+                fence_proxies();                                            // the parts, and the ring's last readers, in front of the copies
+                if (lane < now)
+                    warp::copy_block(sm100::smem_u32(held + lane * S::kPartFloats),
+                                   parts + (int64_t)(2 * (of.first + c0 + lane) + (c0 + lane == 0 ? 1 : 0)) * S::kPartFloats, S::kPartFloats * 4,
+                                   sm100::smem_u32(&s_join));
+            }
+            if (!sm100::mbar_wait(sm100::smem_u32(&s_join), join_parity) && tid == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
+            join_parity ^= 1;
+#pragma unroll
+            for (int x = 0; x < 2 * NB; ++x) {                              // lane c: part c's weight, by powers of two above the largest so far
+                const int head = x * kWarps + warp_id;
+                const float2 st = lane < now ? *reinterpret_cast<const float2*>(held + lane * S::kPartFloats + 8 * NB * DP + head * 2)
+                                             : make_float2(-INFINITY, 0.f);
+                float t = st.x;
+#pragma unroll
+                for (int e = 1; e < 32; e <<= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, e));
+                t = fmaxf(t, top[x]);
+                const float back = top[x] == -INFINITY ? 0.f : exp2_approx(top[x] - t), w = st.x == -INFINITY ? 0.f : exp2_approx(st.x - t);
+                float all_of = w * st.y;
+#pragma unroll
+                for (int e = 1; e < 32; e <<= 1) all_of += __shfl_xor_sync(0xFFFFFFFFu, all_of, e);
+                sum[x] = sum[x] * back + all_of;
+                top[x] = t;
+                s_weight[head][lane] = w;
+                if (lane == 0) s_total[head] = make_float2(back, sum[x]);
+            }
+            meet();
+#pragma unroll
+            for (int x = 0; x < kMine; ++x) {
+                const int head = sub + x * kHeadsAtOnce;
+                const float back = s_total[head].x;
+                r[x] = make_float4(r[x].x * back, r[x].y * back, r[x].z * back, r[x].w * back);
+#pragma unroll 4
+                for (int c = 0; c < now; ++c) {
+                    const float w = s_weight[head][c];
+                    const float4 v = *reinterpret_cast<const float4*>(held + c * S::kPartFloats + head * DP + quad * 4);
+                    r[x].x += w * v.x;
+                    r[x].y += w * v.y;
+                    r[x].z += w * v.z;
+                    r[x].w += w * v.w;
+                }
+            }
+            meet();
+        }
+#pragma unroll
+        for (int x = 0; x < kMine; ++x) {
+            const int head = sub + x * kHeadsAtOnce;
+            if (head < used) store(of.b, of.h, head, r[x], 1.f / s_total[head].y);
+        }
+        if (tid == 0) counters[of.first] = 0;
+        meet();
     }
 }
 
@@ -456,7 +632,7 @@ cudaError_t launch(const AttentionParams& p, int64_t most_tiles, cudaStream_t st
     if (ctas > most_tiles) ctas = most_tiles;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(S::kAllThreads);
     cfg.dynamicSmemBytes = S::kBytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -516,12 +692,18 @@ cudaError_t launch_paged_attention(const void* q, int64_t q_row, int64_t q_head,
     const int64_t longest = table_width * cache.page_tokens;                // (both below 2^31)
     p.longest = longest < INT32_MAX ? longest : INT32_MAX;
     p.page = cache.page_tokens;
+    // token / page for tokens below 2^31: magic = ceil(2^(31 + s) / page), 2^(s - 1) < page <= 2^s, fits 32 bits
+    int log = 0;
+    while (((int64_t)1 << log) < p.page) ++log;
+    p.page_shift = 31 + log;
+    p.page_magic = (unsigned)((((uint64_t)1 << p.page_shift) + p.page - 1) / p.page);
     p.kv_heads = cache.heads;
     p.dim = cache.head_dim;
     p.group = q_heads / cache.heads;
     p.chunks = (p.group + 8 * column_blocks(p.group, p.dim) - 1) / (8 * column_blocks(p.group, p.dim));
     p.requests = (int)requests;
     p.scale_log2 = scale * 1.4426950408889634f;
+    // a CTA counts its tiles in 32 bits, and the grid has at least as many CTAs as the smallest list that needs them
     int64_t most = (p.longest + kTile - 1) / kTile * p.kv_heads * p.chunks;
     most = most > kMaxCtas ? kMaxCtas : most;
     most = most * requests < 1 ? 1 : most * requests;
