@@ -13,8 +13,6 @@ namespace dps {
 
 namespace {
 
-constexpr int kThreads = 1024;
-
 struct TableParams {
     const int32_t* lengths;
     const int32_t* new_tokens;
@@ -54,59 +52,72 @@ struct Request {
     }
 };
 
-// Exclusive running sum over the block's threads; *total of all.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* s_warp, int64_t* total) {
+// Exclusive running sums of two numbers over the block's threads, and their totals: one barrier.
+struct Pair {
+    int64_t rows, share;
+};
+template <int THREADS>
+__device__ __forceinline__ Pair block_scan(Pair v, Pair* s_warp, Pair* total) {
+    constexpr int kWarps = THREADS / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t upto = v;
-    for (int o = 1; o < 32; o <<= 1) {
-        const int64_t u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-        if (lane >= o) upto += u;
-    }
+    const auto warp_scan = [&](Pair x) {                     // inclusive
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t r = __shfl_up_sync(0xFFFFFFFFu, x.rows, o), t = __shfl_up_sync(0xFFFFFFFFu, x.share, o);
+            if (lane >= o) {
+                x.rows += r;
+                x.share += t;
+            }
+        }
+        return x;
+    };
+    const Pair upto = warp_scan(v);
     if (lane == 31) s_warp[warp] = upto;
     __syncthreads();
-    if (warp == 0) {
-        int64_t w = s_warp[lane];
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t u = __shfl_up_sync(0xFFFFFFFFu, w, o);
-            if (lane >= o) w += u;
-        }
-        s_warp[lane] = w;
-    }
-    __syncthreads();
-    const int64_t before = (warp > 0 ? s_warp[warp - 1] : 0) + upto - v;
-    *total = s_warp[31];
-    __syncthreads();
-    return before;
+    const Pair warps = warp_scan(lane < kWarps ? s_warp[lane] : Pair{0, 0});
+    *total = Pair{__shfl_sync(0xFFFFFFFFu, warps.rows, 31), __shfl_sync(0xFFFFFFFFu, warps.share, 31)};
+    const int64_t rows = __shfl_sync(0xFFFFFFFFu, warps.rows, (warp + 31) & 31), share = __shfl_sync(0xFFFFFFFFu, warps.share, (warp + 31) & 31);
+    return Pair{(warp > 0 ? rows : 0) + upto.rows - v.rows, (warp > 0 ? share : 0) + upto.share - v.share};
 }
 
 // The last of the runs that starts at or before x (their starts never fall).
+template <int THREADS>
 __device__ __forceinline__ int run_of(const int* starts, int x) {
     int at = 0;
 #pragma unroll
-    for (int step = kThreads / 2; step > 0; step >>= 1)
+    for (int step = THREADS / 2; step > 0; step >>= 1)
         if (starts[at + step] <= x) at += step;
     return at;
 }
 
-__global__ void __launch_bounds__(kThreads) extend_block_tables_kernel(const TableParams p) {
-    __shared__ int s_row[kThreads], s_share[kThreads];       // where the runs' rows and granted blocks start, cut off at the ends of the lists
-    __shared__ int64_t s_warp[32];
+// (256 threads for as many requests: 13 requests, one token each, took 5.6 us with 1024 threads and two sums after one another.)
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) extend_block_tables_kernel(const TableParams p) {
+    __shared__ int s_row[THREADS], s_share[THREADS];         // where the runs' rows and granted blocks start, cut off at the ends of the lists
+    __shared__ Pair s_warp[2][THREADS / 32];
+    __shared__ int64_t s_used[THREADS / 32];
     sm100::grid_launch_dependents();
     sm100::grid_dependency_wait();
     const int tid = threadIdx.x;
-    const int per = (p.requests + kThreads - 1) / kThreads;
+    const int per = (p.requests + THREADS - 1) / THREADS;
     const int first = min(tid * per, p.requests), last = min(first + per, p.requests);
-    int64_t rows = 0, all_rows, all_taken;
-    for (int b = first; b < last; ++b) rows += max(p.new_tokens[b], 0);
-    const int64_t row0 = block_scan(rows, s_warp, &all_rows);
     Request r;
-    r.row = row0;
-    r.share = 0;
-    for (int b = first; b < last; ++b) {
-        r.read(p, b);
-        r.pass();
+    Pair all;
+    const auto sums = [&](int64_t row, bool bounded) {       // of this thread's run: its rows, its share with the rows' end respected or not
+        Pair v{0, 0};
+        for (int b = first; b < last; ++b) {
+            r.row = bounded ? row + v.rows : INT64_MIN / 2;  // (rows that never reach the end)
+            r.read(p, b);
+            v.rows += r.added;
+            v.share += r.fresh;
+        }
+        return v;
+    };
+    Pair at = block_scan<THREADS>(sums(0, false), s_warp[0], &all);
+    if (all.rows > p.tokens) {                               // some rows pass the end: their requests take no blocks
+        const int64_t row = at.rows;
+        at = block_scan<THREADS>(sums(row, true), s_warp[1], &all);
     }
-    const int64_t share0 = block_scan(r.share, s_warp, &all_taken);
+    const int64_t row0 = at.rows, share0 = at.share, all_rows = all.rows, all_taken = all.share;
     s_row[tid] = (int)min(row0, p.tokens);
     s_share[tid] = (int)min(share0, p.granted_count);
     __syncthreads();
@@ -127,21 +138,23 @@ __global__ void __launch_bounds__(kThreads) extend_block_tables_kernel(const Tab
             r.pass();
         }
         if (tid == 0) p.token_starts[p.requests] = (int)min(all_rows, (int64_t)INT32_MAX);
-        // the largest end of a request that was served
-        for (int o = 16; o > 0; o >>= 1) used = max(used, __shfl_xor_sync(0xFFFFFFFFu, used, o));
-        if ((tid & 31) == 0) s_warp[tid >> 5] = used;
-        __syncthreads();
-        if (tid < 32) {
-            used = s_warp[tid];
+        if (all_taken <= p.granted_count) {
+            if (tid == 0) p.granted_used[0] = (int)all_taken;
+        } else {                                             // the largest end of a request that was served
             for (int o = 16; o > 0; o >>= 1) used = max(used, __shfl_xor_sync(0xFFFFFFFFu, used, o));
-            if (tid == 0) p.granted_used[0] = (int)used;
+            if ((tid & 31) == 0) s_used[tid >> 5] = used;
+            __syncthreads();
+            if (tid == 0) {
+                for (int w = 0; w < THREADS / 32; ++w) used = max(used, s_used[w]);
+                p.granted_used[0] = (int)used;
+            }
         }
     }
 
-    const int64_t stride = (int64_t)gridDim.x * kThreads, mine = (int64_t)blockIdx.x * kThreads + tid;
+    const int64_t stride = (int64_t)gridDim.x * THREADS, mine = (int64_t)blockIdx.x * THREADS + tid;
     // the granted blocks: into the table
     for (int64_t g = mine; g < p.granted_count && g < all_taken; g += stride) {
-        const int run = run_of(s_share, (int)g);
+        const int run = run_of<THREADS>(s_share, (int)g);
         int b = run * per;
         const int end = min(b + per, p.requests);
         r.row = s_row[run];
@@ -164,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) extend_block_tables_kernel(const Tab
         int position = 0;
         int64_t slot = -1;
         if (t < all_rows) {
-            const int run = run_of(s_row, (int)t);
+            const int run = run_of<THREADS>(s_row, (int)t);
             int b = run * per;
             const int end = min(b + per, p.requests);
             r.row = s_row[run];
@@ -214,19 +227,20 @@ cudaError_t launch_extend_block_tables(const int32_t* lengths, const int32_t* ne
     p.requests = (int)requests;
     p.page = page;
     const int64_t items = tokens > granted_count ? tokens : granted_count;
-    int64_t ctas = (items + kThreads - 1) / kThreads;
+    const int threads = requests <= 256 ? 256 : 1024;
+    int64_t ctas = (items + threads - 1) / threads;
     if (ctas > sm_count()) ctas = sm_count();
     if (ctas < 1) ctas = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads);
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, extend_block_tables_kernel, p);
+    const cudaError_t e = threads == 256 ? cudaLaunchKernelEx(&cfg, extend_block_tables_kernel<256>, p) : cudaLaunchKernelEx(&cfg, extend_block_tables_kernel<1024>, p);
     if (e == cudaSuccess) count_launch();
     return e;
 }
