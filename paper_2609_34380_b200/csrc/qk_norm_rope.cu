@@ -4,11 +4,13 @@
 //   y = x / sqrt(mean(x^2) + eps) * w;  pairs (a, b) -> (a cos - b sin, b cos + a sin);  keys and values to their slot
 //
 // A stream: every element is read once and written once, bound by HBM for prompts and by latency for a few tokens.  A head is
-// a group of LANES lanes (8, 16 or 32: the power of two that covers head_dim / 8), each lane holding 8 neighbouring elements in one
-// 16-byte load; the mean is a butterfly over the group, and the other half of a rotated pair is 8 elements of another lane, which
-// come by shuffle as they were loaded (four words; the norm's factor is the same, the weight is that lane's and loaded once).  A warp
-// serves up to kHeads heads per group of one token: their loads are in flight together, and the token's row of the table and the
-// weights are read once for all of them.  All arithmetic in 32 bits, one rounding at the store.
+// a group of LANES lanes (8, 16 or 32: the power of two that covers head_dim / 8), each lane holding 8 of its elements in two pieces of
+// four: where the head is rotated by halves, four of the lower half and their partners of the upper half, else neighbours.  So a
+// rotated pair is always within a lane, and only the mean needs a butterfly over the group.  With the weights and the rotation a lane's
+// elements are u = (P A - Q B) f and v = (Q C + P D) f, f = 1 / sqrt(mean + eps): A .. D are formed once for all the heads that a warp
+// serves, kHeads per group, all queries or all keys of one token, whose loads are in flight together.  All arithmetic in 32 bits, one
+// rounding at the store.  (With 16-byte pieces of one half, partners by shuffle and weights widened for each head, 8192 tokens of 64 + 8 + 8 heads of
+// 128 took 115 us, bound by the number of instructions.)
 #include "dps_internal.h"
 #include "sm100.cuh"
 #include "step_ops.h"
@@ -38,21 +40,35 @@ struct QkParams {
     unsigned char* v;
     int64_t block_stride, token_stride, head_stride, cache_slots, max_position, tokens;
     int* status;
-    int page, dim, q_heads, kv_heads, rotated, tasks;
+    int page, dim, q_heads, kv_heads, rotated, q_tasks, kv_tasks;        // warps per token: q_tasks + 2 kv_tasks
     float eps;
 };
 
-__device__ __forceinline__ uint4 load16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
-
-template <typename T>
-__device__ __forceinline__ void widen(const uint4& v, float (&x)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// A lane's eight elements of a head, in two pieces of four.
+struct Pieces {
+    uint2 a, b;
+};
+__device__ __forceinline__ Pieces load_pieces(const unsigned char* head, int a, int b) {
+    return Pieces{*reinterpret_cast<const uint2*>(head + a * 2), *reinterpret_cast<const uint2*>(head + b * 2)};
+}
+// ... as the members P and Q of four pairs: the pieces, or, interleaved, even and odd elements.
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ void widen(const Pieces& v, float (&p)[4], float (&q)[4]) {
+    const float2 w[4] = {Half2<T>::unpack(v.a.x), Half2<T>::unpack(v.a.y), Half2<T>::unpack(v.b.x), Half2<T>::unpack(v.b.y)};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 f = Half2<T>::unpack(w[i]);
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
+        p[i] = INTERLEAVED ? w[i].x : i % 2 ? w[i / 2].y : w[i / 2].x;
+        q[i] = INTERLEAVED ? w[i].y : i % 2 ? w[2 + i / 2].y : w[2 + i / 2].x;
     }
+}
+template <typename T, bool INTERLEAVED>
+__device__ __forceinline__ Pieces narrow(const float (&p)[4], const float (&q)[4]) {
+    Pieces v;
+    v.a.x = INTERLEAVED ? Half2<T>::pack(p[0], q[0]) : Half2<T>::pack(p[0], p[1]);
+    v.a.y = INTERLEAVED ? Half2<T>::pack(p[1], q[1]) : Half2<T>::pack(p[2], p[3]);
+    v.b.x = INTERLEAVED ? Half2<T>::pack(p[2], q[2]) : Half2<T>::pack(q[0], q[1]);
+    v.b.y = INTERLEAVED ? Half2<T>::pack(p[3], q[3]) : Half2<T>::pack(q[2], q[3]);
+    return v;
 }
 
 template <typename T, int LANES, bool INTERLEAVED>
@@ -61,104 +77,112 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p
     sm100::grid_dependency_wait();
     constexpr int kGroups = 32 / LANES;                     // heads side by side in a warp
     const int lane = threadIdx.x & 31, chunk = lane % LANES, group = lane / LANES;
-    const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-    const int64_t token = task / p.tasks;
+    const int tasks = p.q_tasks + 2 * p.kv_tasks;
+    const unsigned id = blockIdx.x * kWarps + (threadIdx.x >> 5);       // (below 2^31: checked on the host)
+    const int64_t token = id / tasks;
     if (token >= p.tokens) return;
-    const int first = (int)(task - token * p.tasks) * (kHeads * kGroups) + group;
-    const int heads = p.q_heads + 2 * p.kv_heads;
+    int task = (int)(id % tasks), kind = 0;                 // queries, keys or values
+    if (task >= p.q_tasks) {
+        task -= p.q_tasks;
+        kind = task < p.kv_tasks ? 1 : 2;
+        if (kind == 2) task -= p.kv_tasks;
+    }
     const int64_t slot = p.slots[token];
     if (slot < 0) return;                                   // padding
-    const int position = p.rotated > 0 ? p.positions[token] : 0;
-    if (slot >= p.cache_slots || (p.rotated > 0 && (position < 0 || position >= p.max_position))) {
+    const bool rotates = p.rotated > 0;
+    const int position = rotates ? p.positions[token] : 0;
+    if (slot >= p.cache_slots || (rotates && (position < 0 || position >= p.max_position))) {
         if (lane == 0) atomicExch(p.status, (int)DPS_ERR_DATA);
         return;
     }
-    const bool there = chunk * 8 < p.dim;
+    const bool there = chunk * 8 < p.dim, turns = chunk * 8 < p.rotated;
+    const bool halves = !INTERLEAVED && turns;
+    const int first = halves ? chunk * 4 : chunk * 8, second = halves ? p.rotated / 2 + chunk * 4 : chunk * 8 + 4;
+    const int heads = kind == 0 ? p.q_heads : p.kv_heads, head0 = task * (kHeads * kGroups) + group;
+    const unsigned char* const from =
+        p.qkv + (token * p.qkv_stride + (int64_t)(kind == 0 ? 0 : kind == 1 ? p.q_heads : p.q_heads + p.kv_heads) * p.dim) * 2;
 
-    uint4 raw[kHeads];
+    Pieces raw[kHeads];
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
-        const int head = first + i * kGroups;
-        raw[i] = there && head < heads ? load16(p.qkv + (token * p.qkv_stride + (int64_t)head * p.dim + chunk * 8) * 2)
-                                       : make_uint4(0, 0, 0, 0);
+        const int head = head0 + i * kGroups;
+        raw[i] = there && head < heads ? load_pieces(from + (int64_t)head * p.dim * 2, first, second) : Pieces{make_uint2(0, 0), make_uint2(0, 0)};
     }
-    // the rotation of this lane's elements, and the lane that holds their partners
-    const int half = p.rotated / 2;                         // a multiple of 8
-    const bool turns = chunk * 8 < p.rotated;
-    const bool upper = !INTERLEAVED && chunk * 8 >= half;
-    const int partner = INTERLEAVED || !turns ? lane : upper ? lane - half / 8 : lane + half / 8;
-    constexpr int kAngles = INTERLEAVED ? 4 : 8;
-    float cosine[kAngles], sine[kAngles];
-    if (turns) {
-        const float* row = p.cos_sin + (int64_t)position * p.rotated + (INTERLEAVED ? chunk * 4 : chunk * 8 - (upper ? half : 0));
+    unsigned char* to;                                      // of this token's heads, and how far apart they are
+    int64_t step = p.dim;
+    if (kind == 0) to = p.q_out + token * p.q_out_stride * 2;
+    else {
+        const bool narrow_slot = slot <= UINT32_MAX;
+        const int64_t block = narrow_slot ? (unsigned)slot / (unsigned)p.page : slot / p.page, within = slot - block * p.page;
+        to = (kind == 1 ? p.k : p.v) + (block * p.block_stride + within * p.token_stride) * 2;
+        step = p.head_stride;
+    }
+    if (kind == 2) {
 #pragma unroll
-        for (int i = 0; i < kAngles; i += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(row + i), s = *reinterpret_cast<const float4*>(row + half + i);
-            cosine[i] = c.x, cosine[i + 1] = c.y, cosine[i + 2] = c.z, cosine[i + 3] = c.w;
-            sine[i] = s.x, sine[i + 1] = s.y, sine[i + 2] = s.z, sine[i + 3] = s.w;
+        for (int i = 0; i < kHeads; ++i) {
+            const int head = head0 + i * kGroups;
+            if (there && head < heads) {
+                *reinterpret_cast<uint2*>(to + (head * step + first) * 2) = raw[i].a;
+                *reinterpret_cast<uint2*>(to + (head * step + second) * 2) = raw[i].b;
+            }
+        }
+        return;
+    }
+    float a[4], b[4], c[4], d[4];                           // u = (P a - Q b) f, v = (Q c + P d) f
+    {
+        float wp[4] = {1.f, 1.f, 1.f, 1.f}, wq[4] = {1.f, 1.f, 1.f, 1.f};
+        if (p.q_weight != nullptr && there) widen<T, INTERLEAVED>(load_pieces(kind == 0 ? p.q_weight : p.k_weight, first, second), wp, wq);
+        float cosine[4] = {1.f, 1.f, 1.f, 1.f}, sine[4] = {0.f, 0.f, 0.f, 0.f};
+        if (turns) {
+            const float* const row = p.cos_sin + (int64_t)position * p.rotated + chunk * 4;
+            const float4 x = *reinterpret_cast<const float4*>(row), y = *reinterpret_cast<const float4*>(row + p.rotated / 2);
+            cosine[0] = x.x, cosine[1] = x.y, cosine[2] = x.z, cosine[3] = x.w;
+            sine[0] = y.x, sine[1] = y.y, sine[2] = y.z, sine[3] = y.w;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a[e] = wp[e] * cosine[e];
+            b[e] = wq[e] * sine[e];
+            c[e] = wq[e] * cosine[e];
+            d[e] = wp[e] * sine[e];
         }
     }
-    const int64_t to = (slot / p.page) * p.block_stride + (slot % p.page) * p.token_stride + chunk * 8;
-
+    const float per_element = 1.f / p.dim;
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
-        const int head = first + i * kGroups;               // the same branch for a group, not for a warp: shuffles stay outside
-        const bool is_q = head < p.q_heads, is_v = head >= p.q_heads + p.kv_heads;
-        uint4 other;
-        other.x = __shfl_sync(0xFFFFFFFFu, raw[i].x, partner);
-        other.y = __shfl_sync(0xFFFFFFFFu, raw[i].y, partner);
-        other.z = __shfl_sync(0xFFFFFFFFu, raw[i].z, partner);
-        other.w = __shfl_sync(0xFFFFFFFFu, raw[i].w, partner);
-        float x[8], y[8];
-        widen<T>(raw[i], x);
-        widen<T>(other, y);
+        const int head = head0 + i * kGroups;
+        float x[4], y[4], factor = 1.f;
+        widen<T, INTERLEAVED>(raw[i], x, y);
         if (p.q_weight != nullptr) {
             float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum += x[e] * x[e];
+            for (int e = 0; e < 4; ++e) sum += x[e] * x[e] + y[e] * y[e];
 #pragma unroll
             for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            const float scale = 1.f / sqrtf(sum / p.dim + p.eps);
-            if (there) {
-                const unsigned char* w = is_q ? p.q_weight : p.k_weight;
-                float wx[8], wy[8];
-                widen<T>(load16(w + chunk * 16), wx);
-                widen<T>(load16(w + (chunk + partner - lane) * 16), wy);
+            factor = 1.f / sqrtf(sum * per_element + p.eps);
+        }
+        float u[4], v[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    x[e] = x[e] * scale * wx[e];
-                    y[e] = y[e] * scale * wy[e];
-                }
+        for (int e = 0; e < 4; ++e) {
+            u[e] = x[e] * a[e];
+            v[e] = y[e] * c[e];
+        }
+        if (turns) {                                        // (an infinite element meets no zero elsewhere)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u[e] -= y[e] * b[e];
+                v[e] += x[e] * d[e];
             }
         }
-        if (turns) {
-            if (INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float a = x[2 * e], b = x[2 * e + 1];
-                    x[2 * e] = a * cosine[e % kAngles] - b * sine[e % kAngles];
-                    x[2 * e + 1] = b * cosine[e % kAngles] + a * sine[e % kAngles];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float s = sine[e % kAngles];
-                    x[e] = x[e] * cosine[e % kAngles] + y[e] * (upper ? s : -s);
-                }
-            }
+        for (int e = 0; e < 4; ++e) {
+            u[e] *= factor;
+            v[e] *= factor;
         }
         if (there && head < heads) {
-            uint4 packed = raw[i];
-            if (!is_v) {
-                packed.x = Half2<T>::pack(x[0], x[1]);
-                packed.y = Half2<T>::pack(x[2], x[3]);
-                packed.z = Half2<T>::pack(x[4], x[5]);
-                packed.w = Half2<T>::pack(x[6], x[7]);
-            }
-            unsigned char* at = is_q   ? p.q_out + (token * p.q_out_stride + (int64_t)head * p.dim + chunk * 8) * 2
-                                : is_v ? p.v + (to + (head - p.q_heads - p.kv_heads) * p.head_stride) * 2
-                                       : p.k + (to + (head - p.q_heads) * p.head_stride) * 2;
-            *reinterpret_cast<uint4*>(at) = packed;
+            const Pieces out = narrow<T, INTERLEAVED>(u, v);
+            *reinterpret_cast<uint2*>(to + (head * step + first) * 2) = out.a;
+            *reinterpret_cast<uint2*>(to + (head * step + second) * 2) = out.b;
         }
     }
 }
@@ -166,9 +190,9 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p
 template <typename T, int LANES>
 cudaError_t launch(QkParams p, bool interleaved, cudaStream_t stream) {
     constexpr int kPerTask = kHeads * (32 / LANES);
-    p.tasks = (p.q_heads + 2 * p.kv_heads + kPerTask - 1) / kPerTask;
-    const int64_t ctas = (p.tokens * p.tasks + kWarps - 1) / kWarps;
-    if (ctas > INT32_MAX) return cudaErrorInvalidConfiguration;
+    p.q_tasks = (p.q_heads + kPerTask - 1) / kPerTask;
+    p.kv_tasks = (p.kv_heads + kPerTask - 1) / kPerTask;
+    const int64_t ctas = (p.tokens * (p.q_tasks + 2 * p.kv_tasks) + kWarps - 1) / kWarps;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(kThreads);
@@ -220,7 +244,7 @@ cudaError_t launch_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t tok
     p.q_heads = q_heads;
     p.kv_heads = cache.heads;
     p.rotated = rotated;
-    p.tasks = 0;
+    p.q_tasks = p.kv_tasks = 0;                             // the launch knows how many heads a warp serves
     p.eps = eps;
     return cache.type == DPS_TYPE_FP16 ? launch_typed<__half>(p, interleaved, stream) : launch_typed<__nv_bfloat16>(p, interleaved, stream);
 }

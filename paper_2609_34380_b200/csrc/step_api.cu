@@ -76,8 +76,8 @@ dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t T, int3
     if (T > 1 && (qkv_stride < row || q_out_stride < q_row)) return DPS_ERR_SHAPE;
     if (T > 1 && (qkv_stride > INT64_MAX / 4 / T || q_out_stride > INT64_MAX / 4 / T)) return DPS_ERR_SHAPE;
     if (T > 1 && (qkv_stride % 8 != 0 || q_out_stride % 8 != 0)) return DPS_ERR_ALIGN;
-    // a warp serves at least four heads of a token, a block eight warps
-    if (T * ((row / cache->head_dim + 3) / 4) / 8 >= kLimit - 1) return DPS_ERR_SHAPE;
+    // warps are numbered in 31 bits; one serves at least four query, key or value heads of a token
+    if (T * (((int64_t)q_heads + 3) / 4 + 2 * (((int64_t)cache->heads + 3) / 4)) >= kLimit - 64) return DPS_ERR_SHAPE;
     if (T == 0) return DPS_OK;
     if (!qkv || !slots || (q_heads > 0 && !q_out)) return DPS_ERR_NULL;
     if (rotated > 0 && (!positions || !cos_sin)) return DPS_ERR_NULL;
