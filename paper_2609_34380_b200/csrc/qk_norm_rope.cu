@@ -7,7 +7,7 @@
 // a group of LANES lanes (8, 16 or 32: the power of two that covers head_dim / 8), each lane holding 8 of its elements in two pieces of
 // four: where the head is rotated by halves, four of the lower half and their partners of the upper half, else neighbours.  So a
 // rotated pair is always within a lane, and only the mean needs a butterfly over the group.  With the weights and the rotation a lane's
-// elements are u = (P A - Q B) f and v = (Q C + P D) f, f = 1 / sqrt(mean + eps): A .. D are formed once for all the heads that a warp
+// elements are u = (P A + Q B) f and v = (Q C + P D) f, f = 1 / sqrt(mean + eps): A .. D are formed once for all the heads that a warp
 // serves, kHeads per group, all queries or all keys of one token, whose loads are in flight together.  All arithmetic in 32 bits, one
 // rounding at the store.  (With 16-byte pieces of one half, partners by shuffle and weights widened for each head, 8192 tokens of 64 + 8 + 8 heads of
 // 128 took 115 us, bound by the number of instructions.)
@@ -43,6 +43,28 @@ struct QkParams {
     int page, dim, q_heads, kv_heads, rotated, q_tasks, kv_tasks;        // warps per token: q_tasks + 2 kv_tasks
     float eps;
 };
+
+// Two 32-bit values that one instruction works on.
+struct Two {
+    unsigned long long v;
+    Two() = default;
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ float2 both() const {
+        float2 f;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+        return f;
+    }
+};
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two fma2(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
 
 // A lane's eight elements of a head, in two pieces of four.
 struct Pieces {
@@ -87,26 +109,28 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p
         kind = task < p.kv_tasks ? 1 : 2;
         if (kind == 2) task -= p.kv_tasks;
     }
+    // All that does not hang on anything else is asked for at once: a warp's life is the latency of two loads, its row and then the rotation's.
     const int64_t slot = p.slots[token];
-    if (slot < 0) return;                                   // padding
     const bool rotates = p.rotated > 0;
     const int position = rotates ? p.positions[token] : 0;
-    if (slot >= p.cache_slots || (rotates && (position < 0 || position >= p.max_position))) {
-        if (lane == 0) atomicExch(p.status, (int)DPS_ERR_DATA);
-        return;
-    }
     const bool there = chunk * 8 < p.dim, turns = chunk * 8 < p.rotated;
     const bool halves = !INTERLEAVED && turns;
     const int first = halves ? chunk * 4 : chunk * 8, second = halves ? p.rotated / 2 + chunk * 4 : chunk * 8 + 4;
     const int heads = kind == 0 ? p.q_heads : p.kv_heads, head0 = task * (kHeads * kGroups) + group;
-    const unsigned char* const from =
-        p.qkv + (token * p.qkv_stride + (int64_t)(kind == 0 ? 0 : kind == 1 ? p.q_heads : p.q_heads + p.kv_heads) * p.dim) * 2;
-
+    const unsigned char* from = p.qkv + (token * p.qkv_stride + (int64_t)((kind == 0 ? 0 : kind == 1 ? p.q_heads : p.q_heads + p.kv_heads) + head0) * p.dim) * 2;
+    const int live = there ? (heads - head0 + kGroups - 1) / kGroups : 0;        // this lane's heads, up to kHeads of them
     Pieces raw[kHeads];
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
-        const int head = head0 + i * kGroups;
-        raw[i] = there && head < heads ? load_pieces(from + (int64_t)head * p.dim * 2, first, second) : Pieces{make_uint2(0, 0), make_uint2(0, 0)};
+        raw[i] = i < live ? load_pieces(from, first, second) : Pieces{make_uint2(0, 0), make_uint2(0, 0)};
+        from += kGroups * p.dim * 2;
+    }
+    float wp[4] = {1.f, 1.f, 1.f, 1.f}, wq[4] = {1.f, 1.f, 1.f, 1.f};
+    if (p.q_weight != nullptr && there && kind < 2) widen<T, INTERLEAVED>(load_pieces(kind == 0 ? p.q_weight : p.k_weight, first, second), wp, wq);
+    if (slot < 0) return;                                   // padding
+    if (slot >= p.cache_slots || (rotates && (position < 0 || position >= p.max_position))) {
+        if (lane == 0) atomicExch(p.status, (int)DPS_ERR_DATA);
+        return;
     }
     unsigned char* to;                                      // of this token's heads, and how far apart they are
     int64_t step = p.dim;
@@ -117,21 +141,22 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p
         to = (kind == 1 ? p.k : p.v) + (block * p.block_stride + within * p.token_stride) * 2;
         step = p.head_stride;
     }
+    to += (head0 * step + first) * 2;
+    step *= kGroups * 2;
+    const int apart = (second - first) * 2;
     if (kind == 2) {
 #pragma unroll
         for (int i = 0; i < kHeads; ++i) {
-            const int head = head0 + i * kGroups;
-            if (there && head < heads) {
-                *reinterpret_cast<uint2*>(to + (head * step + first) * 2) = raw[i].a;
-                *reinterpret_cast<uint2*>(to + (head * step + second) * 2) = raw[i].b;
+            if (i < live) {
+                *reinterpret_cast<uint2*>(to) = raw[i].a;
+                *reinterpret_cast<uint2*>(to + apart) = raw[i].b;
             }
+            to += step;
         }
         return;
     }
-    float a[4], b[4], c[4], d[4];                           // u = (P a - Q b) f, v = (Q c + P d) f
+    Two a[2], b[2], c[2], d[2];                             // u = (P a + Q b) f, v = (Q c + P d) f
     {
-        float wp[4] = {1.f, 1.f, 1.f, 1.f}, wq[4] = {1.f, 1.f, 1.f, 1.f};
-        if (p.q_weight != nullptr && there) widen<T, INTERLEAVED>(load_pieces(kind == 0 ? p.q_weight : p.k_weight, first, second), wp, wq);
         float cosine[4] = {1.f, 1.f, 1.f, 1.f}, sine[4] = {0.f, 0.f, 0.f, 0.f};
         if (turns) {
             const float* const row = p.cos_sin + (int64_t)position * p.rotated + chunk * 4;
@@ -140,50 +165,45 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const QkParams p
             sine[0] = y.x, sine[1] = y.y, sine[2] = y.z, sine[3] = y.w;
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            a[e] = wp[e] * cosine[e];
-            b[e] = wq[e] * sine[e];
-            c[e] = wq[e] * cosine[e];
-            d[e] = wp[e] * sine[e];
+        for (int e = 0; e < 2; ++e) {
+            const Two w(wp[2 * e], wp[2 * e + 1]), z(wq[2 * e], wq[2 * e + 1]), cs(cosine[2 * e], cosine[2 * e + 1]), sn(sine[2 * e], sine[2 * e + 1]);
+            a[e] = w * cs;
+            b[e] = z * sn * Two(-1.f, -1.f);
+            c[e] = z * cs;
+            d[e] = w * sn;
         }
     }
     const float per_element = 1.f / p.dim;
 #pragma unroll
     for (int i = 0; i < kHeads; ++i) {
-        const int head = head0 + i * kGroups;
         float x[4], y[4], factor = 1.f;
         widen<T, INTERLEAVED>(raw[i], x, y);
+        const Two px[2] = {Two(x[0], x[1]), Two(x[2], x[3])}, py[2] = {Two(y[0], y[1]), Two(y[2], y[3])};
         if (p.q_weight != nullptr) {
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum += x[e] * x[e] + y[e] * y[e];
+            const Two squares = fma2(px[0], px[0], fma2(px[1], px[1], fma2(py[0], py[0], py[1] * py[1])));
+            const float2 halves_of = squares.both();
+            float sum = halves_of.x + halves_of.y;
 #pragma unroll
             for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            factor = 1.f / sqrtf(sum * per_element + p.eps);
+            factor = rsqrtf(sum * per_element + p.eps);
         }
         float u[4], v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            u[e] = x[e] * a[e];
-            v[e] = y[e] * c[e];
-        }
-        if (turns) {                                        // (an infinite element meets no zero elsewhere)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u[e] -= y[e] * b[e];
-                v[e] += x[e] * d[e];
+        for (int e = 0; e < 2; ++e) {
+            Two s = px[e] * a[e], t = py[e] * c[e];
+            if (turns) {                                    // (an infinite element meets no zero elsewhere)
+                s = fma2(py[e], b[e], s);
+                t = fma2(px[e], d[e], t);
             }
+            const float2 f = (s * Two(factor, factor)).both(), g = (t * Two(factor, factor)).both();
+            u[2 * e] = f.x, u[2 * e + 1] = f.y, v[2 * e] = g.x, v[2 * e + 1] = g.y;
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            u[e] *= factor;
-            v[e] *= factor;
-        }
-        if (there && head < heads) {
+        if (i < live) {
             const Pieces out = narrow<T, INTERLEAVED>(u, v);
-            *reinterpret_cast<uint2*>(to + (head * step + first) * 2) = out.a;
-            *reinterpret_cast<uint2*>(to + (head * step + second) * 2) = out.b;
+            *reinterpret_cast<uint2*>(to) = out.a;
+            *reinterpret_cast<uint2*>(to + apart) = out.b;
         }
+        to += step;
     }
 }
 

@@ -213,39 +213,64 @@ __device__ __forceinline__ void load_logits(const T* at, int count, float (&x)[P
     }
 }
 
+// Descending, by exchanges in pairs (a bitonic network).
+template <int PER>
+__device__ __forceinline__ void sort_down(unsigned (&key)[PER]) {
+#pragma unroll
+    for (int size = 2; size <= PER; size *= 2)
+#pragma unroll
+        for (int step = size / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if ((i & step) == 0) {
+                    const unsigned x = key[i], y = key[i + step];
+                    key[i] = (i & size) == 0 ? max(x, y) : min(x, y);
+                    key[i + step] = (i & size) == 0 ? min(x, y) : max(x, y);
+                }
+}
+
+// A lane's values are sorted once, with the expert's number in the lane (the lower the larger) in their lowest bits: a choice then costs a
+// maximum, a ballot and a step in one lane's list.  The bits are no loss to FP16 and BF16 logits, whose 32-bit forms end in zeros.
 template <typename T, int PER>
-__global__ void __launch_bounds__(kThreads) route_experts_kernel(const RouteParams p) {
+__global__ void __launch_bounds__(kThreads, PER <= 8 ? 8 : 4) route_experts_kernel(const RouteParams p) {
     sm100::grid_launch_dependents();
     sm100::grid_dependency_wait();
+    constexpr unsigned kIndex = PER - 1;                    // PER is a power of two
+    constexpr float kCut = PER * 1.2e-7f;                   // what the lowest bits may take from a value, relative to it
     const int lane = threadIdx.x & 31;
     const int first = min(lane * p.per_lane, p.experts), count = min(p.per_lane, p.experts - first);
-    float bias[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) bias[i] = p.bias != nullptr && i < count ? p.bias[first + i] : 0.f;
     const bool by_groups = p.top_groups < p.groups, direct = p.bias == nullptr && !by_groups;
     const int group = p.group_lanes > 0 ? lane / p.group_lanes : 0;
+    float bias[PER], odd_bias = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        bias[i] = p.bias != nullptr && i < count ? p.bias[first + i] : 0.f;
+        odd_bias += bias[i] * 0.f;                          // NaN from one that is not finite
+    }
+    const bool never = (by_groups && p.group_lanes == 0) || odd_bias != 0.f;         // (NaN differs from 0)
 
     for (int64_t token = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5); token < p.tokens; token += (int64_t)gridDim.x * kWarps) {
-        float x[PER];
-        load_logits<T, PER>(static_cast<const T*>(p.logits) + token * p.stride + first, count, x);
-        bool odd = by_groups && p.group_lanes == 0;         // this row is none for 32 bits
-        float top = -INFINITY;
+        const T* const row = static_cast<const T*>(p.logits) + token * p.stride;
+        float x[PER], odd = 0.f;
+        load_logits<T, PER>(row + first, count, x);
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (i < count) {
-                odd |= !(fabsf(x[i]) < INFINITY) || !(fabsf(bias[i]) < INFINITY);
-                top = fmaxf(top, x[i]);
-            }
-        if (__any_sync(kAll, odd)) {
+        for (int i = 0; i < PER; ++i) odd += x[i] * 0.f;
+        if (__any_sync(kAll, never || odd != 0.f)) {
             route_in_64_bits<T, PER>(p, token);
             continue;
         }
-        top = from_ordered(__reduce_max_sync(kAll, ordered(top)));
-        float scale = 1.f, bound = 4e-6f;                   // softmax: 1 / sum;  on the error of a choice value, besides its own rounding
+        float top = 0.f, scale = 1.f, bound = 5e-7f;        // softmax: the largest logit, 1 / sum;  on the error of a score
         unsigned key[PER];
+        if (!p.sigmoid) {
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (i < count) top = fmaxf(top, x[i]);
+            top = from_ordered(__reduce_max_sync(kAll, ordered(top)));
+        }
         if (direct && (p.sigmoid || p.renormalise)) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = i < count ? ordered(x[i]) : 0u;
+            for (int i = 0; i < PER; ++i) key[i] = ordered(x[i]);
         } else {
             float score[PER], sum = 0.f;
 #pragma unroll
@@ -257,85 +282,63 @@ __global__ void __launch_bounds__(kThreads) route_experts_kernel(const RoutePara
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
                 scale = 1.f / sum;
-                bound *= scale;                             // (the largest score)
+                bound = 2e-6f * scale;                      // (the largest score is scale; the smaller ones are off by less)
             }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = i < count ? ordered(direct ? x[i] : score[i] * scale + bias[i]) : 0u;
+            for (int i = 0; i < PER; ++i) key[i] = ordered(direct ? x[i] : score[i] * scale + bias[i]);
         }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) key[i] = i < count ? (key[i] & ~kIndex) | (kIndex - i) : 0u;
+        sort_down<PER>(key);
         bool close = false;
         if (by_groups) {
-            float one = -INFINITY, two = -INFINITY;         // the two largest of the lane, then of its group
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (i < count) {
-                    const float c = from_ordered(key[i]);
-                    two = fmaxf(two, fminf(one, c));
-                    one = fmaxf(one, c);
-                }
+            float one = key[0] != 0u ? from_ordered(key[0]) : -INFINITY, two = PER > 1 && key[PER > 1] != 0u ? from_ordered(key[PER > 1]) : -INFINITY;
             for (int o = 1; o < p.group_lanes; o <<= 1) {
                 const float a = __shfl_xor_sync(kAll, one, o), b = __shfl_xor_sync(kAll, two, o);
                 two = fmaxf(fmaxf(two, b), fminf(one, a));
                 one = fmaxf(one, a);
             }
-            const float worth = two == -INFINITY ? one : one + two;
+            const bool single = two == -INFINITY;
+            const float worth = single ? one : one + two, near = 4.f * bound + (2.f * kCut + 1e-6f) * (fabsf(one) + (single ? 0.f : fabsf(two)));
             int better = 0;                                 // groups in front of this one
             for (int g = 0; g < p.groups; ++g) {
                 const float other = __shfl_sync(kAll, worth, g * p.group_lanes);
-                if (g != group) {
-                    better += other > worth;
-                    close |= fabsf(other - worth) <= 2.f * bound + 1e-6f * (fabsf(one) + fabsf(two == -INFINITY ? 0.f : two));
-                }
+                better += other > worth;
+                close |= g != group && fabsf(other - worth) <= near;
             }
+            close &= group < p.groups;
             if (better >= p.top_groups) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i) key[i] = 0u;
             }
-            close = __any_sync(kAll, close && group < p.groups);
         }
-        unsigned mine = 0u;                                 // the lane's best
-#pragma unroll
-        for (int i = 0; i < PER; ++i) mine = max(mine, key[i]);
-        int taken = -1;                                     // lane j keeps choice j
-        float logit = 0.f, last = 0.f;
+        int taken = 0;                                      // lane j keeps choice j
+        float last = INFINITY;
         for (int j = 0; j <= p.top_k; ++j) {
-            const unsigned best = __reduce_max_sync(kAll, mine);
+            const unsigned best = __reduce_max_sync(kAll, key[0] & ~kIndex);
             if (best == 0u) break;                          // (behind the last choice: no other expert is left)
-            const float value = from_ordered(best), gap = last - value;
-            if (j > 0) close |= direct ? gap > 0.f && gap < 1e-9f : gap <= 2.f * bound + 2e-7f * (fabsf(value) + fabsf(last));
+            const float value = from_ordered(best), gap = last - value, error = kCut * (fabsf(value) + fabsf(last));
+            if (j > 0) close |= direct ? (gap > 0.f && gap < 1e-9f) || (sizeof(T) == 4 && gap <= error) : gap <= 2.f * bound + error + 2e-7f * fabsf(value);
             last = value;
             if (j == p.top_k) break;
-            const int owner = __ffs(__ballot_sync(kAll, mine == best)) - 1;
-            int at = 0;
-            float v = 0.f;
+            const int owner = __ffs(__ballot_sync(kAll, (key[0] & ~kIndex) == best)) - 1;
+            const int at = owner * p.per_lane + (int)(kIndex - (__shfl_sync(kAll, key[0], owner) & kIndex));
+            if (lane == j) taken = at;
             if (lane == owner) {
-                mine = 0u;
 #pragma unroll
-                for (int i = PER - 1; i >= 0; --i)
-                    if (key[i] == best) {                   // the first of equal ones
-                        at = i;
-                        v = x[i];
-                    }
-#pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    if (i == at) key[i] = 0u;
-                    mine = max(mine, key[i]);
-                }
-            }
-            at = __shfl_sync(kAll, at, owner);
-            v = __shfl_sync(kAll, v, owner);
-            if (lane == j) {
-                taken = owner * p.per_lane + at;
-                logit = v;
+                for (int i = 0; i + 1 < PER; ++i) key[i] = key[i + 1];
+                key[PER - 1] = 0u;
             }
         }
         // the weights: of the choices alone if they are divided by their sum
         const bool chosen = lane < p.top_k;
+        const float logit = chosen ? widen(row[taken]) : 0.f;
         const float low = from_ordered(__reduce_min_sync(kAll, chosen ? ordered(logit) : 0xFFFFFFFFu)),
                     high = from_ordered(__reduce_max_sync(kAll, chosen ? ordered(logit) : 0u));
         // scores that 64 bits cannot tell apart (1 - e^-x beyond 16), or that vanish
         if (p.sigmoid) close |= (direct && high >= 16.f) || low <= -60.f;
         else close |= low - top <= -60.f;
-        if (close) {
+        if (__any_sync(kAll, close)) {
             route_in_64_bits<T, PER>(p, token);
             continue;
         }
@@ -359,7 +362,7 @@ __global__ void __launch_bounds__(kThreads) route_experts_kernel(const RoutePara
 template <typename T>
 cudaError_t launch(const RouteParams& p, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    const int64_t ctas = (p.tokens + kWarps - 1) / kWarps, resident = (int64_t)sm_count() * 12;
+    const int64_t ctas = (p.tokens + kWarps - 1) / kWarps, resident = (int64_t)sm_count() * 8;
     cfg.gridDim = dim3((unsigned)(ctas < resident ? ctas : resident));
     cfg.blockDim = dim3(kThreads);
     cfg.stream = stream;
