@@ -31,6 +31,7 @@ constexpr int kWarps = 4;             // that compute; further ones copy
 constexpr int kThreads = kWarps * 32;
 constexpr int kTile = 64;             // tokens of a tile
 constexpr int kWarpTokens = 16;       // ... of them a warp's
+constexpr int kUnitCost = 1;          // what the end of a (request, head) costs, in tiles
 constexpr int kMaxCtas = 1024;        // counters in the workspace
 
 // Workspace: header, a counter per CTA, two parts per CTA.
@@ -60,18 +61,26 @@ __device__ __forceinline__ float exp2_approx(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Orders this thread's view of memory, shared and global, in front of the bulk copies that it issues next.
-__device__ __forceinline__ void fence_proxies() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// Adds one; the counter's value before.  What this thread has seen is seen by whoever counts after it.
+__device__ __forceinline__ unsigned count_in(unsigned* counter) {
+    unsigned before;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+    return before;
+}
 __device__ __forceinline__ int clamped_length(const AttentionParams& p, int b) {
     const int n = p.lengths[b];
     return n <= 0 ? 0 : (int64_t)n > p.longest ? (int)p.longest : n;
 }
 __device__ __forceinline__ int tiles_of(int length) { return (int)(((unsigned)length + kTile - 1) / kTile); }
+// Places that a (request, head) takes in the list: its tiles, and those that stand for its end.
+__device__ __forceinline__ int places_of(int tiles) { return tiles > 0 ? tiles + kUnitCost : 0; }
 
 // A place in the list of tiles.
 struct Place {
     int b, h, j, tiles, length;    // request, key-value head (and chunk of its queries), tile of them; the request's tiles and tokens
+    int rel;                       // how far into the run
     __device__ __forceinline__ void next_unit(const AttentionParams& p, int heads) {
+        rel += places_of(tiles) - j;
         j = 0;
         if (++h < heads) return;
         h = 0;
@@ -80,7 +89,14 @@ struct Place {
         tiles = tiles_of(length);
     }
     __device__ __forceinline__ void next(const AttentionParams& p, int heads) {
-        if (++j == tiles) next_unit(p, heads);
+        if (j + 1 == tiles) next_unit(p, heads);
+        else {
+            ++j;
+            ++rel;
+        }
+    }
+    // whether next() stays below `length` places
+    __device__ __forceinline__ bool goes_on(int length) const { return rel + 1 + (j + 1 == tiles ? kUnitCost : 0) < length;
     }
 };
 
@@ -137,11 +153,10 @@ __global__ void __launch_bounds__((Shape<DP, NB>::kAllThreads), (Shape<DP, NB>::
 paged_attention_kernel(const AttentionParams p) {
     using S = Shape<DP, NB>;
     extern __shared__ __align__(1024) unsigned char smem[];                 // the rows are aligned to their size
-    __shared__ __align__(8) uint64_t s_full[kWarps][S::kStages], s_empty[kWarps][S::kStages], s_join;
+    __shared__ __align__(8) uint64_t s_full[kWarps][S::kStages], s_empty[kWarps][S::kStages];
     __shared__ int64_t s_scan[kWarps];
     __shared__ unsigned s_mask[kWarps][S::kStages];
-    __shared__ float2 s_stat[kWarps][8], s_total[8 * NB];
-    __shared__ float s_weight[8 * NB][32];
+    __shared__ float2 s_stat[kWarps][8];
     __shared__ Place s_first;
     __shared__ int s_flag[2];
 
@@ -152,7 +167,6 @@ paged_attention_kernel(const AttentionParams p) {
             sm100::mbar_init(sm100::smem_u32(&s_full[warp_id][i]), 33);     // 32 lanes' copies and the mask
             sm100::mbar_init(sm100::smem_u32(&s_empty[warp_id][i]), 1);
         }
-        if (warp_id == 0) sm100::mbar_init(sm100::smem_u32(&s_join), 1);
         sm100::fence_barrier_init();
     }
     __syncwarp();
@@ -166,7 +180,7 @@ paged_attention_kernel(const AttentionParams p) {
     const int per = (p.requests + kThreads - 1) / kThreads;
     const int first_request = min(tid * per, p.requests), last_request = warp_id < kWarps ? min(first_request + per, p.requests) : first_request;
     int64_t mine = 0;
-    for (int b = first_request; b < last_request; ++b) mine += tiles_of(clamped_length(p, b));
+    for (int b = first_request; b < last_request; ++b) mine += places_of(tiles_of(clamped_length(p, b)));
     int64_t upto = mine;
     for (int o = 1; o < 32; o <<= 1) {
         const int64_t u = __shfl_up_sync(0xFFFFFFFFu, upto, o);
@@ -195,33 +209,38 @@ paged_attention_kernel(const AttentionParams p) {
             int b = first_request;
             int64_t from = before;
             int length = clamped_length(p, b), tiles = tiles_of(length);
-            while (at >= from + tiles && b + 1 < last_request) {
-                from += tiles;
+            while (at >= from + places_of(tiles) && b + 1 < last_request) {
+                from += places_of(tiles);
                 length = clamped_length(p, ++b);
                 tiles = tiles_of(length);
             }
             const int64_t inside = start - from * heads;
-            const int h = narrow ? (int)inside / tiles : (int)(inside / tiles);
-            s_first = Place{b, h, (int)(inside - (int64_t)h * tiles), tiles, length};
+            const int places = places_of(tiles), h = narrow ? (int)inside / places : (int)(inside / places);
+            Place first{b, h, (int)(inside - (int64_t)h * places), tiles, length, 0};
+            if (first.j >= tiles) {                                         // behind the last tile: the next one's first
+                if (places - first.j < count) first.next_unit(p, heads);
+                else first.rel = count;
+            }
+            s_first = first;
         }
     }
     // requests without tokens: zeros; a length that is none
-    const auto look_for_empty = [&] {
+    const auto look_for_empty = [&](int thread, int threads) {
         for (int b = cta; b < p.requests; b += ctas) {
             const int n = p.lengths[b];
-            if (tid == 0 && (n < 0 || (int64_t)n > p.longest)) atomicExch(p.status, (int)DPS_ERR_DATA);
+            if (thread == 0 && (n < 0 || (int64_t)n > p.longest)) atomicExch(p.status, (int)DPS_ERR_DATA);
             if (n <= 0 || p.longest == 0) {
                 const int64_t row = (int64_t)p.kv_heads * p.group * p.dim / 8;
                 uint4* to = reinterpret_cast<uint4*>(p.out) + b * row;
-                for (int64_t i = tid; i < row; i += kThreads) to[i] = make_uint4(0, 0, 0, 0);
+                for (int64_t i = thread; i < row; i += threads) to[i] = make_uint4(0, 0, 0, 0);
             }
         }
     };
-    if (count == 0) {
-        if (warp_id < kWarps) look_for_empty();
+    __syncthreads();
+    if (count == 0 || s_first.rel >= count) {                               // no tile
+        look_for_empty(tid, S::kAllThreads);
         return;
     }
-    __syncthreads();
 
     // ---- the warps that copy: each serves kServed of the others, 16 tokens of every tile for each
     if (warp_id >= kWarps) {
@@ -255,7 +274,7 @@ paged_attention_kernel(const AttentionParams p) {
         look_up(true);
         int stage = 0;
         uint32_t parity = 1;                                                // the first round of the ring waits for nobody
-        for (int done = 0; done < count; ++done) {
+        for (bool more_tiles = true; more_tiles;) {
             int64_t off[kLooks];
             unsigned wanted[kLooks];
 #pragma unroll
@@ -265,7 +284,8 @@ paged_attention_kernel(const AttentionParams p) {
                 off[l] = known ? (id[l] * p.block_stride + within[l] * p.token_stride + head_off) * 2 : 0;
                 wanted[l] = __ballot_sync(0xFFFFFFFFu, known);
             }
-            if (done + 1 < count) {
+            more_tiles = at.goes_on(count);
+            if (more_tiles) {
                 at.next(p, heads);
                 look_up(false);
             }
@@ -306,6 +326,7 @@ paged_attention_kernel(const AttentionParams p) {
                 parity ^= 1;
             }
         }
+        look_for_empty(tid - kThreads, S::kAllThreads - kThreads);          // (while the others are still computing)
         warp::copies_wait();
         return;
     }
@@ -334,7 +355,6 @@ paged_attention_kernel(const AttentionParams p) {
     float o[NB][DP / 16][4], m[NB][2], l[NB][2];
     Place at = s_first;
     if (S::kQueriesAhead) fetch_queries(at, q_next);
-    look_for_empty();
     bool fresh = true;                                                      // a (request, head) starts here
     const bool from_start = at.j == 0;                                      // the run's first one starts with it
     bool first_unit = true, lost = false;                                   // lost: a copy did not arrive in time
@@ -366,7 +386,8 @@ paged_attention_kernel(const AttentionParams p) {
 
     int stage = 0;
     uint32_t parity = 0;
-    for (int done = 0; done < count; ++done) {
+    for (bool more_tiles = true; more_tiles;) {
+        more_tiles = at.goes_on(count);
         if (fresh) {
             fresh = false;
             if (!S::kQueriesAhead) fetch_queries(at, qf);
@@ -384,7 +405,7 @@ paged_attention_kernel(const AttentionParams p) {
                 m[nb][0] = m[nb][1] = -INFINITY;
                 l[nb][0] = l[nb][1] = 0.f;
             }
-            if (S::kQueriesAhead && done + at.tiles - at.j < count) {
+            if (S::kQueriesAhead && at.rel + places_of(at.tiles) - at.j < count) {
                 Place soon = at;
                 soon.next_unit(p, heads);
                 fetch_queries(soon, q_next);
@@ -458,7 +479,7 @@ paged_attention_kernel(const AttentionParams p) {
 
         // ---- the end of a (request, head), or of the run
         const bool ends = at.j == at.tiles - 1;
-        if (ends || done + 1 == count) {
+        if (ends || !more_tiles) {
             const bool starts_here = !first_unit || from_start;
             const bool whole = ends && starts_here;
             // the stage just read is this warp's until it hands it back: its sums for the others, element d of a head at d ^ (head / 2 % 4 * 8),
@@ -468,7 +489,7 @@ paged_attention_kernel(const AttentionParams p) {
             };
             float* const part = parts + (int64_t)(2 * cta + (starts_here ? 1 : 0)) * S::kPartFloats;
             if (!whole) {                                                   // its first and last tile in the list, and their CTAs
-                const int64_t unit = start + done - at.j, unit_last = unit + at.tiles - 1, big = (int64_t)more * (each + 1);
+                const int64_t unit = start + at.rel - at.j, unit_last = unit + at.tiles - 1, big = (int64_t)more * (each + 1);
                 Split of;
                 of.first = (int)(unit < big ? unit / (each + 1) : more + (unit - big) / each);
                 of.last = (int)(unit_last < big ? unit_last / (each + 1) : more + (unit_last - big) / each);
@@ -520,93 +541,72 @@ paged_attention_kernel(const AttentionParams p) {
             stage = 0;
             parity ^= 1;
         }
-        if (done + 1 < count) at.next(p, heads);
+        if (more_tiles) at.next(p, heads);
     }
     if (lost && lane == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
 
     // ---- the splits that this CTA holds a part of: whoever comes last joins the parts, in their order
     if (head_split.last < 0 && tail_split.last < 0) return;
-    __threadfence();
     meet();
     if (tid < 2) {
         const Split of = tid == 0 ? head_split : tail_split;
-        s_flag[tid] = of.last >= 0 && atomicAdd(&counters[of.first], 1u) == (unsigned)(of.last - of.first);
+        // (the CTA's part, which the barrier has put in front of this, goes with it for all of the GPU)
+        s_flag[tid] = of.last >= 0 && count_in(&counters[of.first]) == (unsigned)(of.last - of.first);
     }
     meet();
-    uint32_t join_parity = 0;
 #pragma unroll 1
     for (int i = 0; i < 2; ++i) {
         if (!s_flag[i]) continue;
-        __threadfence();
         const Split of = i == 0 ? head_split : tail_split;
         const int n = of.last - of.first + 1, used = heads_of(of.h);
-        // As many parts at a time as the ring holds (nobody else copies any more), each by one bulk copy: they are in flight together, and asking for
-        // them costs one instruction (by 16-byte copies, with all threads asking, the 37 parts of a long request took 7 us).
-        constexpr int kAtOnce = S::kBytes / (S::kPartFloats * 4) < 32 ? S::kBytes / (S::kPartFloats * 4) : 32;
-        constexpr int kMine = 8 * NB / kHeadsAtOnce;                        // heads of a thread
-        const float* const held = reinterpret_cast<const float*>(smem);
-        float4 r[kMine];
-#pragma unroll
-        for (int x = 0; x < kMine; ++x) r[x] = make_float4(0.f, 0.f, 0.f, 0.f);
-        float top[2 * NB], sum[2 * NB];                                     // of this warp's heads, running
-#pragma unroll
-        for (int x = 0; x < 2 * NB; ++x) top[x] = -INFINITY, sum[x] = 0.f;
+        // kAtOnce parts at a time, their maxima and totals and their sums asked for together.  (One part after another, the 37 parts of a long request took
+        // 14 us; as bulk copies into shared memory, which want a fence between the two kinds of access, 6.)
+        constexpr int kMine = 8 * NB / kHeadsAtOnce, kAtOnce = kMine <= 2 ? 16 : DP == 256 ? 8 : 4;   // heads of a thread
+        constexpr int kTeam = kQuads < 32 ? kQuads : 32;                    // neighbouring lanes that serve the same head: lane c of them weighs part c
+        const auto part_of = [&](int c) { return parts + (int64_t)(2 * (of.first + c) + (c == 0 ? 1 : 0)) * S::kPartFloats; };
+        Joined r[kMine];
+#pragma unroll 1
         for (int c0 = 0; c0 < n; c0 += kAtOnce) {
-            const int now = min(kAtOnce, n - c0);
-            if (warp_id == 0) {
-                if (lane == 0) sm100::mbar_arrive_expect_tx(sm100::smem_u32(&s_join), now * S::kPartFloats * 4);
-                __syncwarp();
-                fence_proxies();                                            // the parts, and the ring's last readers, in front of the copies
-                if (lane < now)
-                    warp::copy_block(sm100::smem_u32(held + lane * S::kPartFloats),
-                                   parts + (int64_t)(2 * (of.first + c0 + lane) + (c0 + lane == 0 ? 1 : 0)) * S::kPartFloats, S::kPartFloats * 4,
-                                   sm100::smem_u32(&s_join));
+            const int member = lane % kTeam, left = n - c0;
+            float2 st[kMine];
+            float4 v[kAtOnce][kMine];
+#pragma unroll
+            for (int x = 0; x < kMine; ++x)
+                st[x] = __ldcg(reinterpret_cast<const float2*>(part_of(c0 + min(member, left - 1)) + 8 * NB * DP + (sub + x * kHeadsAtOnce) * 2));
+#pragma unroll
+            for (int c = 0; c < kAtOnce; ++c) {
+                const float* const from = part_of(c0 + min(c, left - 1)) + sub * DP + quad * 4;
+#pragma unroll
+                for (int x = 0; x < kMine; ++x) v[c][x] = __ldcg(reinterpret_cast<const float4*>(from + x * kHeadsAtOnce * DP));
             }
-            if (!sm100::mbar_wait(sm100::smem_u32(&s_join), join_parity) && tid == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
-            join_parity ^= 1;
-#pragma unroll
-            for (int x = 0; x < 2 * NB; ++x) {                              // lane c: part c's weight, by powers of two above the largest so far
-                const int head = x * kWarps + warp_id;
-                const float2 st = lane < now ? *reinterpret_cast<const float2*>(held + lane * S::kPartFloats + 8 * NB * DP + head * 2)
-                                             : make_float2(-INFINITY, 0.f);
-                float t = st.x;
-#pragma unroll
-                for (int e = 1; e < 32; e <<= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, e));
-                t = fmaxf(t, top[x]);
-                const float back = top[x] == -INFINITY ? 0.f : exp2_approx(top[x] - t), w = st.x == -INFINITY ? 0.f : exp2_approx(st.x - t);
-                float all_of = w * st.y;
-#pragma unroll
-                for (int e = 1; e < 32; e <<= 1) all_of += __shfl_xor_sync(0xFFFFFFFFu, all_of, e);
-                sum[x] = sum[x] * back + all_of;
-                top[x] = t;
-                s_weight[head][lane] = w;
-                if (lane == 0) s_total[head] = make_float2(back, sum[x]);
-            }
-            meet();
 #pragma unroll
             for (int x = 0; x < kMine; ++x) {
-                const int head = sub + x * kHeadsAtOnce;
-                const float back = s_total[head].x;
-                r[x] = make_float4(r[x].x * back, r[x].y * back, r[x].z * back, r[x].w * back);
-#pragma unroll 4
-                for (int c = 0; c < now; ++c) {
-                    const float w = s_weight[head][c];
-                    const float4 v = *reinterpret_cast<const float4*>(held + c * S::kPartFloats + head * DP + quad * 4);
-                    r[x].x += w * v.x;
-                    r[x].y += w * v.y;
-                    r[x].z += w * v.z;
-                    r[x].w += w * v.w;
+                if (member >= min(left, kAtOnce)) st[x] = make_float2(-INFINITY, 0.f);
+                float top = st[x].x;
+#pragma unroll
+                for (int e = 1; e < kTeam; e <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, e));
+                r[x].rescale(top);
+                const float w = st[x].x == -INFINITY ? 0.f : exp2_approx(st[x].x - r[x].m);      // (a NaN in the sums stays one)
+                float total_of = w * st[x].y;
+#pragma unroll
+                for (int e = 1; e < kTeam; e <<= 1) total_of += __shfl_xor_sync(0xFFFFFFFFu, total_of, e);
+                r[x].l += total_of;
+#pragma unroll
+                for (int c = 0; c < kAtOnce; ++c) {
+                    const float f = __shfl_sync(0xFFFFFFFFu, w, lane / kTeam * kTeam + c);
+                    if (c < left) {
+                        r[x].o.x += f * v[c][x].x;
+                        r[x].o.y += f * v[c][x].y;
+                        r[x].o.z += f * v[c][x].z;
+                        r[x].o.w += f * v[c][x].w;
+                    }
                 }
             }
-            meet();
         }
 #pragma unroll
-        for (int x = 0; x < kMine; ++x) {
-            const int head = sub + x * kHeadsAtOnce;
-            if (head < used) store(of.b, of.h, head, r[x], 1.f / s_total[head].y);
-        }
-        if (tid == 0) counters[of.first] = 0;
-        meet();
+        for (int x = 0; x < kMine; ++x)
+            if (sub + x * kHeadsAtOnce < used) store(of.b, of.h, sub + x * kHeadsAtOnce, r[x].o, 1.f / r[x].l);
+        if (tid == 0) counters[of.first] = 0;                               // ready for the next call
     }
 }
 
