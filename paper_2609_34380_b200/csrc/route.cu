@@ -44,32 +44,29 @@ __device__ __forceinline__ float widen(float v) { return v; }
 __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
 __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 
-// The larger value, of equal ones the lower index, of the whole warp; index INT_MAX where there is none.
-__device__ __forceinline__ void warp_best(double& value, int& index) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const double v = __shfl_xor_sync(kAll, value, o);
-        const int i = __shfl_xor_sync(kAll, index, o);
-        if (i != INT32_MAX && (index == INT32_MAX || v > value || (v == value && i < index))) {
-            value = v;
-            index = i;
-        }
-    }
+// Numbers as whole numbers in their order; 0 is below all of them.  (v + 0 makes one of the two zeros.)
+__device__ __forceinline__ uint64_t ordered(double v) {
+    const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+    return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
+    const unsigned high = __reduce_max_sync(kAll, (unsigned)(v >> 32));
+    const unsigned low = __reduce_max_sync(kAll, (unsigned)(v >> 32) == high ? (unsigned)v : 0u);
+    return (uint64_t)high << 32 | low;
 }
 
-// One row in 64 bits, whatever it holds; lane i has experts i, i + 32, ..
+// One row in 64 bits, whatever it holds.  Lane i has p.per_lane neighbouring experts, as below, so that of equal values the lower lane's is the lower index.
 template <typename T, int PER>
 __device__ __noinline__ void route_in_64_bits(const RouteParams& p, int64_t token) {
     const int lane = threadIdx.x & 31;
+    const int first = min(lane * p.per_lane, p.experts), count = min(p.per_lane, p.experts - first);
     const T* row = static_cast<const T*>(p.logits) + token * p.stride;
 
-    double score[PER], choice[PER];
-    double top = -INFINITY;
+    double score[PER], top = -INFINITY;
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = i * 32 + lane;
-        score[i] = e < p.experts ? (double)widen(row[e]) : -INFINITY;
+        score[i] = i < count ? (double)widen(row[first + i]) : -INFINITY;
         bad |= score[i] != score[i];
         top = fmax(top, score[i]);
     }
@@ -81,22 +78,24 @@ __device__ __noinline__ void route_in_64_bits(const RouteParams& p, int64_t toke
         double sum = 0.0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            score[i] = i * 32 + lane < p.experts ? exp(score[i] - top) : 0.0;
+            score[i] = i < count ? exp(score[i] - top) : 0.0;
             sum += score[i];
         }
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
 #pragma unroll
         for (int i = 0; i < PER; ++i) score[i] /= sum;
     }
-    unsigned open = 0;                                      // this lane's experts that may be taken
+    uint64_t key[PER];                                      // 0: none, or not to be taken any more
+    double one = -INFINITY, two = -INFINITY;                // the lane's two largest choice values
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = i * 32 + lane;
-        choice[i] = score[i];
-        if (e < p.experts) {
-            if (p.bias != nullptr) choice[i] += (double)p.bias[e];
-            bad |= choice[i] != choice[i];
-            open |= 1u << i;
+        key[i] = 0;
+        if (i < count) {
+            const double c = p.bias != nullptr ? score[i] + (double)p.bias[first + i] : score[i];
+            bad |= c != c;
+            key[i] = ordered(c);
+            two = fmax(two, fmin(one, c));
+            one = fmax(one, c);
         }
     }
     const auto give_up = [&] {
@@ -112,56 +111,69 @@ __device__ __noinline__ void route_in_64_bits(const RouteParams& p, int64_t toke
     if (p.top_groups < p.groups) {
         const int size = p.experts / p.groups;
         double worth = -INFINITY;                           // of group `lane`
-        for (int g = 0; g < p.groups; ++g) {
-            double one = -INFINITY, two = -INFINITY;        // the two largest of it
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = i * 32 + lane;
-                if (e < p.experts && e / size == g) {
-                    two = fmax(two, fmin(one, choice[i]));
-                    one = fmax(one, choice[i]);
-                }
-            }
-            for (int o = 16; o > 0; o >>= 1) {
+        if (p.group_lanes > 0) {
+            for (int o = 1; o < p.group_lanes; o <<= 1) {
                 const double a = __shfl_xor_sync(kAll, one, o), b = __shfl_xor_sync(kAll, two, o);
                 two = fmax(fmax(two, b), fmin(one, a));
                 one = fmax(one, a);
             }
-            if (lane == g) worth = size > 1 ? one + two : one;
+            worth = __shfl_sync(kAll, size > 1 ? one + two : one, lane * p.group_lanes & 31);
+        } else {
+            for (int g = 0; g < p.groups; ++g) {
+                one = two = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (i < count && first + i >= g * size && first + i < (g + 1) * size) {
+                        const double c = p.bias != nullptr ? score[i] + (double)p.bias[first + i] : score[i];
+                        two = fmax(two, fmin(one, c));
+                        one = fmax(one, c);
+                    }
+                for (int o = 16; o > 0; o >>= 1) {
+                    const double a = __shfl_xor_sync(kAll, one, o), b = __shfl_xor_sync(kAll, two, o);
+                    two = fmax(fmax(two, b), fmin(one, a));
+                    one = fmax(one, a);
+                }
+                if (lane == g) worth = size > 1 ? one + two : one;
+            }
         }
-        if (__any_sync(kAll, worth != worth)) return give_up();     // +Inf and -Inf among the choices
+        if (__any_sync(kAll, lane < p.groups && worth != worth)) return give_up();       // +Inf and -Inf among the choices
+        uint64_t value = lane < p.groups ? ordered(worth) : 0;
         unsigned kept = 0;
         for (int j = 0; j < p.top_groups; ++j) {
-            double v = worth;
-            int g = lane < p.groups && !((kept >> lane) & 1u) ? lane : INT32_MAX;
-            warp_best(v, g);
+            const uint64_t best = warp_max(value);
+            const int g = __ffs(__ballot_sync(kAll, value == best)) - 1;
             kept |= 1u << g;
+            if (lane == g) value = 0;
         }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = i * 32 + lane;
-            if (e < p.experts && !((kept >> (e / size)) & 1u)) open &= ~(1u << i);
-        }
+        for (int i = 0; i < PER; ++i)
+            if (i < count && !((kept >> ((first + i) / size)) & 1u)) key[i] = 0;
     }
     double sum = 0.0, mine = 0.0;                           // lane j keeps choice j
     int taken = -1;
     for (int j = 0; j < p.top_k; ++j) {
-        double v = 0.0, s = 0.0;
-        int at = INT32_MAX;
+        uint64_t local = 0;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (((open >> i) & 1u) && (at == INT32_MAX || choice[i] > v)) {
-                v = choice[i];
+        for (int i = 0; i < PER; ++i) local = max(local, key[i]);
+        const uint64_t best = warp_max(local);
+        const int owner = __ffs(__ballot_sync(kAll, local == best)) - 1;
+        int at = 0;
+        double s = 0.0;
+#pragma unroll
+        for (int i = PER - 1; i >= 0; --i)
+            if (key[i] == best) {                           // the first of equal ones
+                at = i;
                 s = score[i];
-                at = i * 32 + lane;
             }
-        int e = at;
-        warp_best(v, e);
-        const int owner = e & 31;
+        if (lane == owner) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (i == at) key[i] = 0;
+        }
+        at = __shfl_sync(kAll, at, owner);
         s = __shfl_sync(kAll, s, owner);
-        if (lane == owner) open &= ~(1u << (e >> 5));
         if (lane == j) {
-            taken = e;
+            taken = owner * p.per_lane + at;
             mine = s;
         }
         sum += s;
@@ -299,36 +311,44 @@ __global__ void __launch_bounds__(kThreads, PER <= 8 ? 8 : 4) route_experts_kern
                 one = fmaxf(one, a);
             }
             const bool single = two == -INFINITY;
-            const float worth = single ? one : one + two, near = 4.f * bound + (2.f * kCut + 1e-6f) * (fabsf(one) + (single ? 0.f : fabsf(two)));
+            const float worth = single ? one : one + two, size = fabsf(one) + (single ? 0.f : fabsf(two));
             int better = 0;                                 // groups in front of this one
-            for (int g = 0; g < p.groups; ++g) {
-                const float other = __shfl_sync(kAll, worth, g * p.group_lanes);
-                better += other > worth;
-                close |= g != group && fabsf(other - worth) <= near;
-            }
-            close &= group < p.groups;
-            if (better >= p.top_groups) {
+#pragma unroll 4
+            for (int g = 0; g < p.groups; ++g) better += __shfl_sync(kAll, worth, g * p.group_lanes) > worth;
+            const bool live = group < p.groups, kept = live && better < p.top_groups;
+            // the border between the groups that stay and those that go: too near, or the place of several equal ones
+            const float in = from_ordered(__reduce_min_sync(kAll, kept ? ordered(worth) : 0xFFFFFFFFu)),
+                        out = from_ordered(__reduce_max_sync(kAll, live && !kept ? ordered(worth) : 0u)),
+                        most = from_ordered(__reduce_max_sync(kAll, live ? ordered(size) : 0u));
+            close = in - out <= 4.f * bound + (2.f * kCut + 1e-6f) * most || __popc(__ballot_sync(kAll, kept)) != p.top_groups * p.group_lanes;
+            if (!kept) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i) key[i] = 0u;
             }
         }
-        int taken = 0;                                      // lane j keeps choice j
-        float last = INFINITY;
-        for (int j = 0; j <= p.top_k; ++j) {
+        unsigned won = 0u;                                  // lane j keeps choice j: its key, and the lane that it comes from
+        int from = 0;
+        for (int j = 0; j < p.top_k; ++j) {
             const unsigned best = __reduce_max_sync(kAll, key[0] & ~kIndex);
-            if (best == 0u) break;                          // (behind the last choice: no other expert is left)
-            const float value = from_ordered(best), gap = last - value, error = kCut * (fabsf(value) + fabsf(last));
-            if (j > 0) close |= direct ? (gap > 0.f && gap < 1e-9f) || (sizeof(T) == 4 && gap <= error) : gap <= 2.f * bound + error + 2e-7f * fabsf(value);
-            last = value;
-            if (j == p.top_k) break;
             const int owner = __ffs(__ballot_sync(kAll, (key[0] & ~kIndex) == best)) - 1;
-            const int at = owner * p.per_lane + (int)(kIndex - (__shfl_sync(kAll, key[0], owner) & kIndex));
-            if (lane == j) taken = at;
+            const unsigned got = __shfl_sync(kAll, key[0], owner);
+            if (lane == j) {
+                won = got;
+                from = owner;
+            }
             if (lane == owner) {
 #pragma unroll
                 for (int i = 0; i + 1 < PER; ++i) key[i] = key[i + 1];
                 key[PER - 1] = 0u;
             }
+        }
+        const int taken = from * p.per_lane + (int)(kIndex - (won & kIndex));
+        {                                                   // every choice against the one behind it, the last one against the best that is left (0: none)
+            const unsigned rest = __reduce_max_sync(kAll, key[0] & ~kIndex), after = __shfl_down_sync(kAll, won, 1);
+            const unsigned below = (lane == p.top_k - 1 ? rest : after) & ~kIndex;
+            const float value = from_ordered(won & ~kIndex), other = from_ordered(below), gap = value - other, error = kCut * (fabsf(value) + fabsf(other));
+            close |= lane < p.top_k && below != 0u &&
+                     (direct ? (gap > 0.f && gap < 1e-9f) || (sizeof(T) == 4 && gap <= error) : gap <= 2.f * bound + error + 2e-7f * fabsf(value));
         }
         // the weights: of the choices alone if they are divided by their sum
         const bool chosen = lane < p.top_k;
