@@ -692,11 +692,7 @@ cudaError_t launch_paged_attention(const void* q, int64_t q_row, int64_t q_head,
     const int64_t longest = table_width * cache.page_tokens;                // (both below 2^31)
     p.longest = longest < INT32_MAX ? longest : INT32_MAX;
     p.page = cache.page_tokens;
-    // token / page for tokens below 2^31: magic = ceil(2^(31 + s) / page), 2^(s - 1) < page <= 2^s, fits 32 bits
-    int log = 0;
-    while (((int64_t)1 << log) < p.page) ++log;
-    p.page_shift = 31 + log;
-    p.page_magic = (unsigned)((((uint64_t)1 << p.page_shift) + p.page - 1) / p.page);
+    page_division(p.page, p.page_magic, p.page_shift);
     p.kv_heads = cache.heads;
     p.dim = cache.head_dim;
     p.group = q_heads / cache.heads;

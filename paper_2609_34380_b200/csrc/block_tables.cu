@@ -26,6 +26,9 @@ struct TableParams {
     int32_t* granted_used;
     int* status;
     int requests, page;
+    unsigned page_magic, page_shift;        // n / page = n * page_magic >> page_shift, for n below 2^31
+    __device__ __forceinline__ int pages(int n) const { return (int)(((uint64_t)(unsigned)n * page_magic) >> page_shift); }
+    __device__ __forceinline__ int pages_up(int n) const { return n > 0 ? pages(n - 1) + 1 : 0; }
 };
 
 // One request: what it has, what it adds, where its shares start.
@@ -40,10 +43,11 @@ struct Request {
         const int m = p.new_tokens[b];
         added = m < 0 ? 0 : m;
         const int64_t after = (int64_t)length + m;
-        const int64_t pages = (after + p.page - 1) / p.page;
-        valid = length >= 0 && m >= 0 && after <= INT32_MAX && pages <= p.table_width && (added == 0 || row + added <= p.tokens);
-        have = valid ? (int)(((int64_t)length + p.page - 1) / p.page) : 0;
-        fresh = valid ? (int)pages - have : 0;
+        valid = length >= 0 && m >= 0 && after <= INT32_MAX && (added == 0 || row + added <= p.tokens);
+        const int need = valid ? p.pages_up((int)after) : 0;
+        valid &= need <= p.table_width;
+        have = valid ? p.pages_up(length) : 0;
+        fresh = valid ? need - have : 0;
     }
     __device__ __forceinline__ bool served(const TableParams& p) const { return valid && (fresh == 0 || share + fresh <= p.granted_count); }
     __device__ __forceinline__ void pass() {
@@ -189,10 +193,10 @@ __global__ void __launch_bounds__(THREADS) extend_block_tables_kernel(const Tabl
             }
             if (b < end && r.served(p)) {
                 position = r.length + (int)(t - r.row);
-                const int index = position / p.page;
+                const int index = p.pages(position);
                 // the entries behind `have` may be written by another CTA just now: they are read where they come from
                 const int block = index < r.have ? p.table[b * p.table_stride + index] : p.granted[r.share + index - r.have];
-                if ((uint32_t)block < (uint64_t)p.blocks) slot = (int64_t)block * p.page + position % p.page;
+                if ((uint32_t)block < (uint64_t)p.blocks) slot = (int64_t)block * p.page + (position - index * p.page);
                 else bad = true;
             }
         }
@@ -226,6 +230,7 @@ cudaError_t launch_extend_block_tables(const int32_t* lengths, const int32_t* ne
     p.status = status;
     p.requests = (int)requests;
     p.page = page;
+    page_division(page, p.page_magic, p.page_shift);
     const int64_t items = tokens > granted_count ? tokens : granted_count;
     const int threads = requests <= 256 ? 256 : 1024;
     int64_t ctas = (items + threads - 1) / threads;

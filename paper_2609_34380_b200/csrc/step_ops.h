@@ -9,6 +9,14 @@
 
 namespace dps {
 
+// n / page = n * magic >> shift for every n below 2^31: with 2^(s - 1) < page <= 2^s, magic = ceil(2^(31 + s) / page) fits 32 bits.
+inline void page_division(int32_t page, unsigned& magic, unsigned& shift) {
+    int log = 0;
+    while (((int64_t)1 << log) < page) ++log;
+    shift = 31 + log;
+    magic = (unsigned)((((uint64_t)1 << shift) + page - 1) / page);
+}
+
 cudaError_t launch_extend_block_tables(const int32_t* lengths, const int32_t* new_tokens, int64_t requests, const int32_t* granted,
                                        int64_t granted_count, int32_t* table, int64_t table_stride, int64_t table_width, int32_t page,
                                        int64_t blocks, int32_t* lengths_out, int32_t* token_starts, int32_t* positions, int64_t* slots,
