@@ -106,7 +106,7 @@ dps_status dps_paged_attention(const void* q, int64_t q_row_stride, int64_t q_he
     if (!(scale - scale == 0.f)) return DPS_ERR_SHAPE;      // Inf, NaN
     // tiles of 64 tokens: a block counts its share of them in 32 bits
     const int64_t longest = table_width * cache->page_tokens < kLimit ? table_width * cache->page_tokens : kLimit;
-    if ((longest / 64 + 1) * q_heads >= ((int64_t)1 << 38) / (B > 0 ? B : 1)) return DPS_ERR_SHAPE;
+    if ((longest / 64 + 2) * q_heads >= ((int64_t)1 << 38) / (B > 0 ? B : 1)) return DPS_ERR_SHAPE;
     if (B == 0) return DPS_OK;
     if (!q || !lengths || !out || (table_width > 0 && !block_table)) return DPS_ERR_NULL;
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lengths, 4)) return DPS_ERR_ALIGN;
