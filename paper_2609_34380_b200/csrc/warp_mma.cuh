@@ -10,7 +10,7 @@ namespace warp {
 
 // 16 bytes global -> shared, past L1; bytes == 0 writes zeros and reads nothing.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.cg.shared.global.L2::64B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // 4 bytes global -> shared.
 __device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
