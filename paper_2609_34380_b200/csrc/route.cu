@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(kThreads, PER <= 8 ? 8 : 4) route_experts_kern
         }
         if (direct && (p.sigmoid || p.renormalise)) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = ordered(x[i]);
+            for (int i = 0; i < PER; ++i) key[i] = ordered(x[i] + 0.f);      // (one of the two zeros)
         } else {
             float score[PER], sum = 0.f;
 #pragma unroll
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, PER <= 8 ? 8 : 4) route_experts_kern
                 bound = 2e-6f * scale;                      // (the largest score is scale; the smaller ones are off by less)
             }
 #pragma unroll
-            for (int i = 0; i < PER; ++i) key[i] = ordered(direct ? x[i] : score[i] * scale + bias[i]);
+            for (int i = 0; i < PER; ++i) key[i] = ordered(direct ? x[i] + 0.f : score[i] * scale + bias[i]);
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) key[i] = i < count ? (key[i] & ~kIndex) | (kIndex - i) : 0u;

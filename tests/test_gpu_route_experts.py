@@ -60,6 +60,18 @@ def test_ties_fall_on_the_lower_index():
             check(few, 8, torch.zeros(64, device=DEV), sigmoid, groups, top_groups)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("E", [8, 32, 64, 256])
+def test_the_two_zeros_are_equal(dtype, E):
+    """A row of zeros of either sign: the first experts, whatever the signs."""
+    logits = torch.zeros((64, E), dtype=dtype, device=DEV)
+    logits[torch.rand((64, E), device=DEV) < 0.5] = -0.0
+    for kw in ({}, {"scoring": dps.DPS_SCORE_SIGMOID}, {"renormalise": False}, {"bias": torch.zeros(E, device=DEV)}):
+        _, experts, weights = dps.dps_route_experts(logits, 4, **kw)
+        assert torch.equal(experts.view(64, 4), torch.arange(4, dtype=torch.int32, device=DEV).expand(64, 4)), kw
+        assert torch.equal(weights, weights[:1, :1].expand(64, 4)), kw
+
+
 def test_choices_that_32_bits_cannot_tell_apart():
     """Scores that differ in the 9th digit: the sum with the bias decides in 64 bits."""
     rng = np.random.default_rng(5)
