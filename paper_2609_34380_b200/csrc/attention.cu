@@ -274,6 +274,7 @@ paged_attention_kernel(const AttentionParams p) {
         look_up(true);
         int stage = 0;
         uint32_t parity = 1;                                                // the first round of the ring waits for nobody
+        bool late = false;                                                  // a stage did not come back in time: no more waits, the lanes stay together
         for (bool more_tiles = true; more_tiles;) {
             int64_t off[kLooks];
             unsigned wanted[kLooks];
@@ -292,11 +293,8 @@ paged_attention_kernel(const AttentionParams p) {
 #pragma unroll
             for (int c = 0; c < kServed; ++c) {
                 const uint32_t full = sm100::smem_u32(&s_full[served + c][stage]);
-                if (!sm100::mbar_wait(sm100::smem_u32(&s_empty[served + c][stage]), parity)) {
-                    if (lane == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
-                    warp::copies_wait();
-                    return;
-                }
+                if (!late && !sm100::mbar_wait(sm100::smem_u32(&s_empty[served + c][stage]), parity)) late = true;
+                __syncwarp();
                 const int64_t c_off = off[c * kWarpTokens / 32];
                 const unsigned mask = (wanted[c * kWarpTokens / 32] >> (c * kWarpTokens % 32)) & 0xFFFFu;
                 if (mask != 0) {
@@ -327,6 +325,7 @@ paged_attention_kernel(const AttentionParams p) {
             }
         }
         look_for_empty(tid - kThreads, S::kAllThreads - kThreads);          // (while the others are still computing)
+        if (late) atomicExch(p.status, (int)DPS_ERR_CUDA);
         warp::copies_wait();
         return;
     }
@@ -543,7 +542,7 @@ paged_attention_kernel(const AttentionParams p) {
         }
         if (more_tiles) at.next(p, heads);
     }
-    if (lost && lane == 0) atomicExch(p.status, (int)DPS_ERR_CUDA);
+    if (lost) atomicExch(p.status, (int)DPS_ERR_CUDA);
 
     // ---- the splits that this CTA holds a part of: whoever comes last joins the parts, in their order
     if (head_split.last < 0 && tail_split.last < 0) return;
