@@ -84,6 +84,8 @@ dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t T, int3
     if ((q_weight == nullptr) != (k_weight == nullptr)) return DPS_ERR_NULL;
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16)) return DPS_ERR_ALIGN;
     if (!aligned(slots, 8) || !aligned(positions, 4)) return DPS_ERR_ALIGN;
+    // in place each warp writes what it has read itself; with other strides it would write another one's
+    if (q_out == qkv && q_heads > 0 && T > 1 && q_out_stride != qkv_stride) return DPS_ERR_DATA;
     int* status;
     const dps_status st = device_status_word(&status);
     if (st != DPS_OK) return st;

@@ -74,6 +74,8 @@ def test_qk_norm_rope():
                        (dict(table=HALF), "ALIGN"), (dict(qw=HALF, kw_=FAKE), "ALIGN"), (dict(slots=ctypes.c_void_p(0x10004)), "ALIGN"), (dict(pos=ODD), "ALIGN"),
                        (dict(T=(1 << 31) - 1, heads=65535, stride=65539 * 64, out_stride=65535 * 64), "SHAPE")]:
         assert call(**kw) == getattr(binding, "DPS_ERR_" + status), kw
+    # queries in place, but in rows of another stride: a warp would write what another one has yet to read
+    assert call(qkv=FAKE, out=FAKE) == binding.DPS_ERR_DATA
     assert call(T=0, qkv=None, slots=None, out=None, pos=None, table=None) == binding.DPS_OK
 
 
