@@ -7,7 +7,8 @@ them, and the requests' lengths.  Block (unit, index) of the manager is block id
 The requests in hand are rows 0 .. n-1 of a batch.  A step gives each of them new tokens (`extend`: the blocks are taken from the
 manager, tables, positions and slots are built by `dps_extend_block_tables`); each layer then writes the step's keys and values
 (`write`: `dps_qk_norm_rope` on the QKV linear's output) and, in a step of one token per request, reads all that there are
-(`attend`: `dps_paged_attention`).  `finish` gives a request's blocks back and moves the last row into its place.
+(`attend`: `dps_paged_attention`).  `finish` gives a request's blocks back and moves the last row into its place.  The tables and
+the workspace are one for all calls, which therefore belong on one stream (or streams that events order).
 """
 from __future__ import annotations
 
@@ -22,7 +23,8 @@ from .sum_manager import Block, SumManager
 
 @dataclass
 class Step:
-    """What one step's kernels read; `single`: every request has one new token, row b of the batch being request b."""
+    """What one step's kernels read; `single`: every request has one new token, row b of the batch being request b.  Good until the next
+    `extend` or `finish`: `lengths` is a view of the cache's own."""
     requests: int
     tokens: int
     single: bool
@@ -104,6 +106,8 @@ class PagedKvCache:
     def finish(self, row: int) -> Optional[int]:
         """The request's blocks go back; the last row takes its place.  Returns that row's former number, None if it was the last itself."""
         last = len(self.lengths) - 1
+        if not 0 <= row <= last:
+            raise ValueError(f"row {row} is none of the {last + 1} requests")
         self.manager.free_kv_blocks(self.held[row])
         moved = None
         if row != last:

@@ -99,12 +99,29 @@ def test_refusals():
     for new, kw in (([1], {}), ([1, -1], {}), ([1, 49], {}), ([5, 5], {"rows": 9})):
         with pytest.raises(ValueError):
             cache.extend(new, **kw)
+    for row in (-1, 2):
+        with pytest.raises(ValueError):
+            cache.finish(row)
+    assert cache.lengths == [0, 0]
     assert cache.extend([40, 40]) is not None and cache.extend([8, 8]) is not None
     cache.finish(0)
     step = cache.extend([0])
     assert step.tokens == 0 and not step.single
     with pytest.raises(ValueError):
         cache.attend(0, step, torch.zeros((1, 4, DIM), dtype=torch.float16, device=DEV))
+
+
+def test_no_requests_and_no_tokens():
+    cache = PagedKvCache(sm.SumManager(2, 4, 0), 1, 4, 4, DIM, PAGE, max_requests=2, max_tokens_per_request=40)
+    for rows in (0, 3):
+        step = cache.extend([], rows=rows)
+        assert step.tokens == 0 and step.slots.tolist() == [-1] * rows and step.starts.tolist() == [0]
+        q = cache.write(0, step, torch.ones((rows, 12 * DIM), dtype=torch.float16, device=DEV))
+        assert q.shape == (rows, 4, DIM) and cache.attend(0, step, q).shape == (0, 4, DIM)
+    cache.admit()
+    step = cache.extend([0], rows=2)
+    cache.write(0, step, torch.ones((2, 12 * DIM), dtype=torch.float16, device=DEV))
+    assert step.lengths.tolist() == [0] and not bool(cache.caches.any()) and dps.dps_stream_status() == dps.DPS_OK
 
 
 def test_a_decoder_step_in_one_graph():
