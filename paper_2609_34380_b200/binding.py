@@ -417,7 +417,7 @@ def dps_extend_block_tables(lengths: torch.Tensor, new_tokens: torch.Tensor, gra
                             stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
     """Block tables of a step, in place, and (lengths_out [B], token_starts [B + 1], positions [T], slots [T], granted_used [1]).
     T is the size of positions and slots, or `tokens` where they are to be made."""
-    if stream is None and _native is not None and granted_used is not None:
+    if stream is None and _native is not None and granted_used is not None and tokens is None:
         out = _native.extend_block_tables(lengths, new_tokens, granted, block_table, page_tokens, blocks, lengths_out, token_starts, positions,
                                           slots, granted_used)
         if out.__class__ is int:

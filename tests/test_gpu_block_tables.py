@@ -155,4 +155,6 @@ def test_refusals():
             ((n, m, g, t, 2 ** 32 + 16, 9), {"tokens": 2}, ValueError), ((n, m, g.cpu(), t, 16, 9), {"tokens": 2}, ValueError)]:
         with pytest.raises(error):
             dps.dps_extend_block_tables(*args, **kw)
+    with pytest.raises(ValueError):                         # outputs given and another number of tokens
+        dps.dps_extend_block_tables(n, m, g, t, 16, 9, dev([0, 0]), dev([0, 0, 0]), dev([0, 0]), dev([0, 0], torch.int64), dev([0]), tokens=3)
     assert dps.dps_launch_count() == launches
