@@ -293,8 +293,10 @@ paged_attention_kernel(const AttentionParams p) {
 #pragma unroll
             for (int c = 0; c < kServed; ++c) {
                 const uint32_t full = sm100::smem_u32(&s_full[served + c][stage]);
-                if (!late && !sm100::mbar_wait(sm100::smem_u32(&s_empty[served + c][stage]), parity)) late = true;
-                __syncwarp();
+                const uint32_t empty = sm100::smem_u32(&s_empty[served + c][stage]);
+                if (!sm100::mbar_try_wait(empty, parity)) {
+                    if (!late && !sm100::mbar_wait(empty, parity)) late = true;
+                }
                 const int64_t c_off = off[c * kWarpTokens / 32];
                 const unsigned mask = (wanted[c * kWarpTokens / 32] >> (c * kWarpTokens % 32)) & 0xFFFFu;
                 if (mask != 0) {
