@@ -11,6 +11,9 @@
 //     values the lower lane's is the lower index.
 //   * top-k: the lanes' best as whole numbers in the floats' order, one warp-wide maximum and one ballot a choice.
 //   * The weights need one accurate exponential a lane: lane j has choice j.
+// 16384 tokens, 256 experts in 8 groups, sigmoid and bias: 26 us, 900 warp instructions a row with the issue slots 64 % busy (10 MB, 1.5 us of HBM; so bound
+// by instructions).  Maxima over all of a lane's values for each choice instead of sorted lists took 58 us, gaps looked over choice by choice (and slower rows in 64 bits) 44; blocks of 32 or 64
+// threads, or one per four tokens, 25.7 to 28.2.  8 tokens of 8 experts: 2.0 us, a launch.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
