@@ -1,8 +1,9 @@
-"""B200-native dual-precision (fast / full mode) linear layers over nested FP8 + residual planes.
+"""B200-native dual-precision (fast / full mode) linear layers over nested FP8 + residual planes, and the operators of a
+decoder step between them.
 
 The computation lives in ``libdps.so`` (hand-written CUDA for sm_100a behind the C ABI declared
-in ``include/dps.h``); ``binding`` exposes the same calls to Python and ``workloads`` draws the
-seeded synthetic inputs.
+in ``include/dps.h``); ``binding`` exposes the same calls to Python, ``kv_cache`` runs the operators over the blocks of
+``sum_manager``, and ``workloads`` draws the seeded synthetic inputs.
 """
 from . import workloads  # noqa: F401
 from .binding import (  # noqa: F401
