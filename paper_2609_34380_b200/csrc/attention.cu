@@ -12,8 +12,8 @@
 //     up one tile ahead, so a page may end anywhere.
 //   * Keys times queries: S^T (16 tokens x 8 heads) = K (16 x dim) Q^T by m16n8k16 products, the tokens being the rows of the
 //     matrix product: up to eight heads that share the keys cost one column block, one head alone does too.  The scores' maximum and sum run along (in 32
-//     bits, by powers of two).  Values: O^T (dim x 8 heads) += V^T P^T, where P is handed over as the sum of two 16-bit values, so
-//     that the weights keep 16 to 22 bits of precision and the result differs from 64-bit sums by its own rounding only.
+//     bits, by powers of two).  Values: O^T (dim x 8 heads) += V^T P^T, where P is handed over as the sum of two 16-bit values: a weight
+//     keeps 16 bits of precision as BF16, 22 as FP16, there down to 2^-39 of the largest weight so far (kLift).  The sums are 32 bits wide.
 //   * At the end of a (request, head) the CTA's four warps are joined through shared memory.  If the run covers only a part of it, the
 //     part goes to the workspace, and the CTA that comes last (a counter per split) joins the parts in their order.
 //
@@ -80,6 +80,11 @@ __device__ __forceinline__ int clamped_length(const AttentionParams& p, int b) {
 __device__ __forceinline__ int tiles_of(int length) { return (int)(((unsigned)length + kTile - 1) / kTile); }
 // Places that a (request, head) takes in the list: its tiles, and those that stand for its end.
 __device__ __forceinline__ int places_of(int tiles) { return tiles > 0 ? tiles + kUnitCost : 0; }
+
+// FP16 ends at 2^-24, and what a long tail of weights below that adds up to is not nothing beside one large weight whose value is small (3000 tokens, 19
+// below the largest score: 13 % of the result were lost).  So all weights are 2^15 times their value, the largest 2^15; the factor goes out with the division by their total.
+template <typename T> constexpr float kLift = 32768.f;
+template <> constexpr float kLift<__nv_bfloat16> = 1.f;
 
 // A place in the list of tiles.
 struct Place {
@@ -455,7 +460,7 @@ paged_attention_kernel(const AttentionParams p) {
                 }
                 float pr[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) pr[e] = exp2_approx(x[e] - top[e & 1]);
+                for (int e = 0; e < 4; ++e) pr[e] = exp2_approx(x[e] - top[e & 1]) * kLift<T>;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) l[nb][e] = l[nb][e] * scale[e] + (pr[e] + pr[e + 2]);
 #pragma unroll
