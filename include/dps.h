@@ -309,7 +309,8 @@ DPS_API dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t
  * (strides q_row_stride, q_head_stride, multiples of 8 elements); out: contiguous [B][q_heads][head_dim].  q_heads is
  * a multiple of cache->heads; B * q_heads * (table_width * page_tokens / 64 + 2) is below 2^38.  Scores, maxima and sums in 32 bits, one rounding at the end; the
  * weights p_t meet the values as sums of two 16-bit numbers, which hold 16 bits of a weight with a BF16 cache, 22 with an FP16 one, there nothing
- * finer than 2^-39 of the largest weight.  Only tokens below the length are read, whatever stands behind them.  lengths[b] == 0 gives zeros.  A length that is negative counts as 0, one beyond table_width * page_tokens as that (status
+ * finer than 2^-39 of the largest weight.  An infinite element of V makes its element of the output that infinity, whatever the token's weight; NaN if
+ * both infinities meet in it, or a NaN.  Only tokens below the length are read, whatever stands behind them.  lengths[b] == 0 gives zeros.  A length that is negative counts as 0, one beyond table_width * page_tokens as that (status
  * word set); the tokens of a block id outside [0, blocks) count for nothing (status word set; a row that has no other gives NaN).
  *
  * The cache's length is split over the GPU, and the parts are joined in a fixed order within the same launch, which takes scratch:

@@ -127,13 +127,52 @@ struct Shape {
     static constexpr int kPartFloats = 8 * NB * (DP + 2);                   // a part: sums, then maximum and total of each head
 };
 
+// Infinite values.  A sum that has met one is NaN where the formula's is infinite: the value is multiplied by the 16-bit remainder of its weight too (zero or
+// negative, for half of all weights), by a weight that 32 bits do not hold, by a rescaling of the sum.  Every weight being positive, the formula's answer hangs
+// on the values alone: the infinity that is there, NaN if both are, or a NaN.  So a thread that has stored a NaN although the weights' total is a number
+// (in the output kOdd stands for it) reads that column once more over its CTA's run, when all tiles of the run are done and before the parts are joined; the
+// factors of the joining are never zero, so that a part's infinity stays one.  In a function of its own this costs finite values 0 to 0.7 % (32 mixed requests 33.97
+// -> 34.10 us; sixteen queries per key 33.8 -> 34.4, 2 %); at the place of the store it was 0.5 to 6 %.  One infinity among 131071 tokens: 0.28 ms instead of 0.09.
+constexpr unsigned kOdd = 0x7FFEu;                                          // a rounded NaN is 0x7FFF in both types
+constexpr float kLeast = 1.17549435e-38f;                                   // 2^-126
+// Ones in the lowest bits of those of a pair that have this magnitude.
+__device__ __forceinline__ unsigned which(unsigned pair, unsigned magnitude) { return __vcmpeq2(pair & 0x7FFF7FFFu, magnitude * 0x10001u) & 0x00010001u; }
+// Of four elements, those that `asked` names (a bit each): the infinity among tokens [from, to) of a request's values, or NaN.
+template <typename T>
+__device__ __forceinline__ void infinities_of(const AttentionParams& p, int b, int kv, int d, int from, int to, unsigned asked, float (&out)[4]) {
+    unsigned up = 0, down = 0;                                              // a NaN counts as both
+    int64_t index = from / p.page, at = from;
+    for (; at < to && (up & down & asked) != asked; ++index) {
+        const int64_t ends = (index + 1) * p.page, stop = ends < to ? ends : to;
+        const int id = p.table[b * p.table_stride + index];
+        if ((unsigned)id < (uint64_t)p.blocks) {
+            const T* v = static_cast<const T*>(p.v) + id * p.block_stride + (at - index * p.page) * p.token_stride + kv * p.head_stride + d;
+#pragma unroll 8
+            for (int n = (int)(stop - at); n > 0; --n, v += p.token_stride) {
+                const uint2 raw = *reinterpret_cast<const uint2*>(v);
+                const float2 x = Half2<T>::unpack(raw.x), y = Half2<T>::unpack(raw.y);
+                const float e[4] = {x.x, x.y, y.x, y.y};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    up |= (unsigned)!(e[i] < INFINITY) << i;
+                    down |= (unsigned)!(e[i] > -INFINITY) << i;
+                }
+            }
+        }
+        at = stop;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (asked >> i & 1u) out[i] = (up ^ down) >> i & 1u ? (up >> i & 1u ? INFINITY : -INFINITY) : NAN;
+}
+
 // Joins `count` running sums of one head and one group of four elements.
 struct Joined {
     float m = -INFINITY, l = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     __device__ __forceinline__ void rescale(float top) {
         if (top > m) {
-            const float w = exp2_approx(m - top);
+            const float w = fmaxf(exp2_approx(m - top), kLeast);
             l *= w;
             o.x *= w;
             o.y *= w;
@@ -159,9 +198,58 @@ struct Split {
     int b = 0, h = 0;
 };
 
+// Of a (key-value head and chunk of its queries): the head, how many queries, where four elements of one of them go.
+__device__ __forceinline__ int kv_of(const AttentionParams& p, int h) { return p.chunks == 1 ? h : h / p.chunks; }
+template <int NB>
+__device__ __forceinline__ int heads_in(const AttentionParams& p, int h) { return p.chunks == 1 ? p.group : min(p.group - h % p.chunks * 8 * NB, 8 * NB); }
+template <typename T, int NB>
+__device__ __forceinline__ uint2* place_of(const AttentionParams& p, int b, int h, int head, int quad) {
+    const int kv = kv_of(p, h);
+    return reinterpret_cast<uint2*>(static_cast<T*>(p.out) + (((int64_t)b * p.kv_heads + kv) * p.group + (h - kv * p.chunks) * 8 * NB + head) * p.dim + quad * 4);
+}
+
+// What one thread has stored of its CTA's run, starting at `at`, with NaN for infinities: elements of the output where the (request, head) is whole, of a part where not.
+template <typename T, int DP, int NB>
+__device__ __noinline__ void settle_infinities(const AttentionParams& p, Place at, int count, float* parts) {
+    constexpr int kQuads = DP / 4, kHeadsAtOnce = kThreads / kQuads;
+    const int quad = threadIdx.x % kQuads, sub = threadIdx.x / kQuads;
+    for (;;) {
+        const int tiles = min(at.tiles - at.j, count - at.rel), from = at.j * kTile;        // of it in this run
+        const int to = (int)min((int64_t)from + (int64_t)tiles * kTile, (int64_t)at.length), kv = kv_of(p, at.h);
+        const bool whole = tiles == at.tiles;
+        float* const part = parts + (int64_t)(2 * blockIdx.x + (at.j == 0 ? 1 : 0)) * Shape<DP, NB>::kPartFloats;
+        for (int head = sub; head < heads_in<NB>(p, at.h) && quad * 4 < p.dim; head += kHeadsAtOnce) {
+            unsigned asked = 0;
+            float value[4];
+            uint2* const place = place_of<T, NB>(p, at.b, at.h, head, quad);
+            float* const sums = part + head * DP + quad * 4;
+            if (whole) {
+                const uint2 packed = *place;
+                const unsigned x = which(packed.x, kOdd), y = which(packed.y, kOdd);
+                asked = (x & 1u) | (x >> 16) << 1 | (y & 1u) << 2 | (y >> 16) << 3;
+                const float2 v = Half2<T>::unpack(packed.x), w = Half2<T>::unpack(packed.y);
+                value[0] = v.x, value[1] = v.y, value[2] = w.x, value[3] = w.y;
+            } else {
+                const float l = part[8 * NB * DP + head * 2 + 1];
+                for (int i = 0; i < 4; ++i) {
+                    value[i] = sums[i];
+                    asked |= (unsigned)(value[i] != value[i] && l < INFINITY) << i;
+                }
+            }
+            if (asked == 0) continue;
+            infinities_of<T>(p, at.b, kv, quad * 4, from, to, asked, value);
+            if (whole) *place = make_uint2(Half2<T>::pack(value[0], value[1]), Half2<T>::pack(value[2], value[3]));
+            else
+                for (int i = 0; i < 4; ++i) sums[i] = value[i];
+        }
+        if (at.rel + places_of(at.tiles) - at.j >= count) return;
+        at.next_unit(p, p.kv_heads * p.chunks);
+    }
+}
+
 template <typename T, int DP, int NB>
 __global__ void __launch_bounds__((Shape<DP, NB>::kAllThreads), (Shape<DP, NB>::kCtas))
-paged_attention_kernel(const AttentionParams p) {
+paged_attention_kernel(const __grid_constant__ AttentionParams p) {
     using S = Shape<DP, NB>;
     extern __shared__ __align__(1024) unsigned char smem[];                 // the rows are aligned to their size
     __shared__ __align__(8) uint64_t s_full[kWarps][S::kStages], s_empty[kWarps][S::kStages];
@@ -170,6 +258,7 @@ paged_attention_kernel(const AttentionParams p) {
     __shared__ float2 s_stat[kWarps][8];
     __shared__ Place s_first;
     __shared__ int s_flag[2];
+    __shared__ bool s_odd[kThreads];                                        // whether the thread has stored a NaN that may be an infinity
 
     sm100::grid_launch_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp_id = tid >> 5;
@@ -379,18 +468,21 @@ paged_attention_kernel(const AttentionParams p) {
     float* const parts = reinterpret_cast<float*>(p.workspace + kHeaderBytes + kCounterBytes);
     constexpr int kQuads = DP / 4, kHeadsAtOnce = kThreads / kQuads;
     const int quad = tid % kQuads, sub = tid / kQuads;
-    auto kv_of = [&](int h) { return p.chunks == 1 ? h : h / p.chunks; };
-    auto heads_of = [&](int h) { return p.chunks == 1 ? p.group : min(p.group - h % p.chunks * 8 * NB, 8 * NB); };
+    auto heads_of = [&](int h) { return heads_in<NB>(p, h); };
     auto store = [&](int b, int h, int head, const float4& v, float factor) {
         if (quad * 4 < p.dim) {
-            T* const out = static_cast<T*>(p.out) +
-                           (((int64_t)b * p.kv_heads + kv_of(h)) * p.group + (h - kv_of(h) * p.chunks) * 8 * NB + head) * p.dim + quad * 4;
             uint2 packed;
             packed.x = Half2<T>::pack(v.x * factor, v.y * factor);
             packed.y = Half2<T>::pack(v.z * factor, v.w * factor);
-            *reinterpret_cast<uint2*>(out) = packed;
+            const uint2 odd = make_uint2(which(packed.x, 0x7FFFu), which(packed.y, 0x7FFFu));
+            if ((odd.x | odd.y) != 0u && factor > 0.f && factor < INFINITY) {
+                packed = make_uint2(packed.x ^ odd.x, packed.y ^ odd.y);
+                s_odd[tid] = true;
+            }
+            *place_of<T, NB>(p, b, h, head, quad) = packed;
         }
     };
+    s_odd[tid] = false;
     auto meet = [] {                                                        // of the computing warps
         __syncwarp();
         sm100::named_barrier_sync(1, kThreads);
@@ -538,6 +630,7 @@ paged_attention_kernel(const AttentionParams p) {
                     }
                     if (whole) store(at.b, at.h, nb * 8 + head, r.o, 1.f / r.l);
                     else {
+                        if (r.o.x != r.o.x || r.o.y != r.o.y || r.o.z != r.o.z || r.o.w != r.o.w) s_odd[tid] = true;
                         *reinterpret_cast<float4*>(part + (nb * 8 + head) * DP + quad * 4) = r.o;
                         if (quad == 0) *reinterpret_cast<float2*>(part + 8 * NB * DP + (nb * 8 + head) * 2) = make_float2(r.m, r.l);
                     }
@@ -556,6 +649,7 @@ paged_attention_kernel(const AttentionParams p) {
         if (more_tiles) at.next(p, heads);
     }
     if (lost) atomicExch(p.status, (int)DPS_ERR_CUDA);
+    if (s_odd[tid]) settle_infinities<T, DP, NB>(p, s_first, count, parts);
 
     // ---- the splits that this CTA holds a part of: whoever comes last joins the parts, in their order
     if (head_split.last < 0 && tail_split.last < 0) return;
@@ -598,7 +692,7 @@ paged_attention_kernel(const AttentionParams p) {
 #pragma unroll
                 for (int e = 1; e < kTeam; e <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, e));
                 r[x].rescale(top);
-                const float w = st[x].x == -INFINITY ? 0.f : exp2_approx(st[x].x - r[x].m);      // (a NaN in the sums stays one)
+                const float w = fmaxf(exp2_approx(st[x].x - r[x].m), kLeast);
                 float total_of = w * st[x].y;
 #pragma unroll
                 for (int e = 1; e < kTeam; e <<= 1) total_of += __shfl_xor_sync(0xFFFFFFFFu, total_of, e);
@@ -617,7 +711,7 @@ paged_attention_kernel(const AttentionParams p) {
         }
 #pragma unroll
         for (int x = 0; x < kMine; ++x)
-            if (sub + x * kHeadsAtOnce < used) store(of.b, of.h, sub + x * kHeadsAtOnce, r[x].o, 1.f / r[x].l);
+            if (sub + x * kHeadsAtOnce < used) store(of.b, of.h, sub + x * kHeadsAtOnce, r[x].o, r[x].l > 0.f ? 1.f / r[x].l : NAN);
         if (tid == 0) counters[of.first] = 0;                               // ready for the next call
     }
 }
