@@ -61,7 +61,7 @@ class PagedKvCache:
 
     def extend(self, new_tokens: Sequence[int], rows: Optional[int] = None) -> Optional[Step]:
         """Room for new_tokens[b] tokens of each request, or None (and no change) if the manager cannot supply the blocks.  `rows`: the
-        step's rows are padded to so many."""
+        step's rows are padded to so many.  A call that raises takes no blocks either."""
         n, total = len(self.lengths), sum(new_tokens)
         if len(new_tokens) != n or any(m < 0 for m in new_tokens):
             raise ValueError(f"one number of new tokens, not negative, for each of the {n} requests")
@@ -76,16 +76,20 @@ class PagedKvCache:
         granted = self.manager.alloc_kv_blocks(sum(fresh))
         if granted is None:
             return None
+        try:
+            ids = [u * self.manager.blocks_per_unit + b for u, b in granted]
+            host = torch.tensor([*new_tokens, *ids], dtype=torch.int32).pin_memory()
+            both = host.to("cuda", non_blocking=True)
+            lengths, starts, positions, slots, _ = binding.dps_extend_block_tables(
+                self._lengths[self._now, :n], both[:n], both[n:], self.block_table[:n], self.page_tokens, self.blocks, self._lengths[self._now ^ 1, :n],
+                granted_used=self._used, tokens=rows)
+        except BaseException:               # no memory for the step, say: nothing was launched, and nobody has the blocks
+            self.manager.free_kv_blocks(granted)
+            raise
         at = 0
         for held, m in zip(self.held, fresh):
             held.extend(granted[at:at + m])
             at += m
-        ids = [u * self.manager.blocks_per_unit + b for u, b in granted]
-        host = torch.tensor([*new_tokens, *ids], dtype=torch.int32).pin_memory()
-        both = host.to("cuda", non_blocking=True)
-        lengths, starts, positions, slots, _ = binding.dps_extend_block_tables(
-            self._lengths[self._now, :n], both[:n], both[n:], self.block_table[:n], self.page_tokens, self.blocks, self._lengths[self._now ^ 1, :n],
-            granted_used=self._used, tokens=rows)
         self._now ^= 1
         self.lengths = after
         return Step(n, total, all(m == 1 for m in new_tokens), lengths, starts, positions, slots)
