@@ -268,12 +268,6 @@ __device__ __forceinline__ float4 ld_cluster_v4_f32(uint32_t addr) {
     return v;
 }
 
-// A warpgroup gives up, or takes, registers of its block: executed by all its warps.  One that takes waits until they are free.
-template <int COUNT>
-__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(COUNT)); }
-template <int COUNT>
-__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(COUNT)); }
-
 // ---- programmatic dependent launch ---------------------------------------------------------------
 // Ask for one line of global memory to be brought into L2.  L2 is the point of coherence for this
 // GPU's own writes, so a line requested before an earlier kernel has finished writing it is still
