@@ -243,7 +243,8 @@ DPS_API dps_status dps_restore_residual(uint8_t* w_resid, const uint8_t* backup_
  * The paper's engine serves these from the system it is built on; here they stand beside the linear layers, so that
  * a step runs from the QKV linear's output to the experts' rows in this library.  None of them synchronises, and none
  * allocates.  They share the conventions above: nothing is enqueued on an error that the host sees, a bad index met
- * on the device sets the status word (DPS_ERR_DATA) and is left out, and the results are deterministic.
+ * on the device sets the status word (DPS_ERR_DATA) and is left out, and the results are deterministic.  Outputs overlap
+ * neither inputs nor one another, but where an operator says that they may.
  */
 typedef enum { DPS_TYPE_FP16 = 0, DPS_TYPE_BF16 = 1, DPS_TYPE_FP32 = 2 } dps_type;
 

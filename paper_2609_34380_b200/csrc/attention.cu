@@ -2,7 +2,8 @@
 //
 //   out[b][h] = sum_t p_t V[t],  p = softmax_t(scale q[b][h] . K[t])
 //
-// Every key and value is read once and takes part in 4 * (heads that share it) operations per element: a stream bound by HBM.
+// Every key and value is read once for up to eight queries that share it (sixteen up to a head size of 128; each further eight or sixteen read it again) and takes
+// part in 4 operations per element and query: a stream bound by HBM.
 // The kernel is built around that stream:
 //   * The work is a flat list of tiles, 64 tokens of one (request, key-value head) each, in that order.  A resident grid cuts it into
 //     equal runs, one per CTA, whatever the lengths are: each CTA sums the lengths itself (they are on the device) and finds its
@@ -17,11 +18,12 @@
 //   * At the end of a (request, head) the CTA's four warps are joined through shared memory.  If the run covers only a part of it, the
 //     part goes to the workspace, and the CTA that comes last (a counter per split) joins the parts in their order.
 //
-// Measured in graphs, against the floor of the bytes at a copy's 6.58 TB/s: one request of 131071 tokens, 64 / 8 heads of 128, 88.9 us (81.6; the
-// same access pattern without arithmetic takes 80.5); 112 requests up to 8190, 60 / 10 heads of 96, 320 (262); 8 requests up to 4096, 64 / 8 heads, 22.0
-// (12.9: the start and the joins take 4.5); 32 requests of 1 to 3001 tokens, 32 / 32 heads, 33.8 (19.5: half of the 992 units have less than 20 tokens, and
-// each unit costs its CTA 1.7 to 2.8 us); one short request 4.7.  Warps that copy for themselves took 101 us for the first of them, a bulk
-// copy per row 134 to 161, registers without shared memory 140.
+// Measured in graphs, three sets of inputs in turn, against the floor of the bytes at a copy's 6.58 TB/s: one request of 131071 tokens, 64 / 8 heads of 128, 88 to
+// 96 us on different GPUs (81.6; the same access pattern without arithmetic takes 80.5); 112 requests up to 8190, 60 / 10 heads of 96, 321 to 360 (262); 8 requests up to 4096,
+// 64 / 8 heads, 22.1 (12.9: the start and the joins take 4.5); 32 requests of 1 to 3001 tokens, 32 / 32 heads, 33.7 (19.5: half of the 992 units have less than
+// 20 tokens, and each unit costs its CTA 1.7 to 2.8 us); one short request 4.7.  Other shapes, 16 requests up to 8192: 32 / 8 heads of 64 29.5 (16.6), 64 / 4 of 128 33.9 (16.7),
+// 96 / 4 of 128, read twice, 54.5 (16.7), 16 / 4 of 256 45.5 (33.2), 64 / 4 of 256, read twice, 85.6 (33.3).  Warps that copy for themselves took 101 us for the
+// 131071 tokens, a bulk copy per row 134 to 161, registers without shared memory 140.
 #include "dps_internal.h"
 #include "sm100.cuh"
 #include "step_ops.h"

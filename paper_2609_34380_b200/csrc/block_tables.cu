@@ -5,7 +5,7 @@
 // bytes, the largest steps a megabyte.  So nothing is exchanged between CTAs: each sums all requests itself (out of L2), keeps the
 // sums of the requests' runs -- one run per thread -- in shared memory, and then serves its share of the three lists (requests, granted
 // blocks, rows), finding the request of an item by bisection of those sums and a walk through one run.
-// 1500 requests, 65536 rows: 7.1 us (pages by division 8.3; 512 threads a block 7.5, 256 8.5); 13 requests, one token each: 3.6.
+// 1500 requests, 65536 rows: 7.2 us in a graph (pages by division 8.3; 512 threads a block 7.5, 256 8.5), 9.0 in a stream; 13 requests, one token each: 3.5.
 #include "dps_internal.h"
 #include "sm100.cuh"
 #include "step_ops.h"

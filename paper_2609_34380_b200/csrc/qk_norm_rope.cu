@@ -11,8 +11,8 @@
 // serves, kHeads per group, all queries or all keys of one token, whose loads are in flight together.  All arithmetic in 32 bits, one
 // rounding at the store.
 //
-// 8192 tokens of 64 + 8 + 8 heads of 128, FP16: 340 MB in 59.7 us, 5.7 TB/s, 87 % of what a copy reaches; 999 tokens of 24 + 6 + 6 heads of 96 4.6 us, one
-// token 2.5 us.  What did not hold: 16-byte pieces of one half, partners by shuffle and weights widened for each head 115 us, bound by the number of
+// 8192 tokens of 64 + 8 + 8 heads of 128, FP16: 340 MB in 59.7 to 65 us with the GPU, 5.2 to 5.7 TB/s, 79 to 87 % of what a copy reaches; 999 tokens of 24 + 6 + 6 heads of 96
+// 4.4 us, one token 2.4 us.  Few heads leave lanes idle: 8192 tokens of 12 + 1 + 1 heads of 96 22.1 us (47 MB, 7.2 us), of 4 + 4 + 4 heads of 80 17.2 (34 MB, 5.2).  What did not hold: 16-byte pieces of one half, partners by shuffle and weights widened for each head 115 us, bound by the number of
 // instructions; loads in the order of their use and arithmetic by single values 79 us; blocks of 256 threads, whose places wait for the slowest of
 // eight warps, 66 us (64 threads 59.6, but 5.1 us for the 999 tokens); three heads a group 70.8 us, five 63.6; several tasks a warp, one after another, 75.
 #include "dps_internal.h"

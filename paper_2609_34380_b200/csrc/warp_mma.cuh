@@ -10,7 +10,7 @@ namespace warp {
 
 // 16 bytes global -> shared, past L1; bytes == 0 writes zeros and reads nothing.  L2 fetches 64 bytes of a line: by default it fetches all
 // 128, and rows of 192 bytes in separate places then bring half a line of their neighbours each (paged attention, 112 requests, 1726 MB of keys
-// and values: 2304 MB read, 352 us; so 1733 MB, 317 us).
+// and values: 2304 MB read, 352 us; so 1733 MB, 317 us on the same GPU).
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t bytes) {
     asm volatile("cp.async.cg.shared.global.L2::64B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
