@@ -277,7 +277,7 @@ typedef struct {
  * A request is left out -- its length and its table row stay as they are, its rows get slot -1, the status word is set --
  * if one of its numbers is negative, if it would pass table_width blocks or 2^31 - 1 tokens, if its rows would pass T, or if `granted`
  * runs out before it is served.  A block id outside [0, blocks) is entered as -1 and its tokens get slot -1 (status too).
- * lengths_out must not be lengths.  B up to 2^20.  All arrays are device memory; granted may be NULL if G == 0.
+ * Outputs that overlap one another, lengths, new_tokens or granted are refused (DPS_ERR_DATA).  B up to 2^20.  All arrays are device memory; granted may be NULL if G == 0.
  */
 DPS_API dps_status dps_extend_block_tables(const int32_t* lengths, const int32_t* new_tokens, int64_t B, const int32_t* granted,
                                            int64_t G, int32_t* block_table, int64_t table_stride, int64_t table_width,

@@ -52,9 +52,21 @@ dps_status dps_extend_block_tables(const int32_t* lengths, const int32_t* new_to
                           (const void*)lengths_out, (const void*)token_starts, (const void*)positions, (const void*)granted_used})
         if (!aligned(p, 4)) return DPS_ERR_ALIGN;
     if (!aligned(slots, 8)) return DPS_ERR_ALIGN;
-    // the inputs are read by every block of the launch while one of them writes the lengths
+    // the inputs are read by every block of the launch while others write the outputs
+    struct Array {
+        const void* at;
+        size_t bytes;
+    };
     const size_t n = (size_t)B * 4;
-    if (B > 0 && (overlap(lengths, n, lengths_out, n) || overlap(new_tokens, n, lengths_out, n))) return DPS_ERR_DATA;
+    const Array inputs[] = {{lengths, n}, {new_tokens, n}, {granted, (size_t)G * 4}};
+    const Array outputs[] = {{lengths_out, n}, {token_starts, n + 4}, {positions, (size_t)T * 4}, {slots, (size_t)T * 8}, {granted_used, 4}};
+    const auto meet = [](const Array& a, const Array& b) { return a.bytes > 0 && b.bytes > 0 && overlap(a.at, a.bytes, b.at, b.bytes); };
+    for (const Array& out : outputs) {
+        for (const Array& in : inputs)
+            if (meet(out, in)) return DPS_ERR_DATA;
+        for (const Array& other : outputs)
+            if (&other != &out && meet(out, other)) return DPS_ERR_DATA;
+    }
     int* status;
     const dps_status st = device_status_word(&status);
     if (st != DPS_OK) return st;

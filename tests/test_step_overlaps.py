@@ -1,0 +1,24 @@
+"""CPU: outputs that lie over inputs or over one another are refused before anything is launched."""
+import ctypes
+
+import pytest
+
+from paper_2609_34380_b200 import binding
+
+FIRST = 0x10000000
+
+
+@pytest.mark.parametrize("out,other", [(o, i) for o in ("after", "starts", "positions", "slots", "used") for i in ("lengths", "new", "granted", "after", "starts", "positions", "slots", "used")
+                                       if o != i])
+def test_extend_block_tables(out, other):
+    """Every output over every other array, by all of it and by its first or last element."""
+    B, G, T = 4, 8, 8
+    size = dict(lengths=4 * B, new=4 * B, granted=4 * G, after=4 * B, starts=4 * (B + 1), positions=4 * T, slots=8 * T, used=4, table=4 * B * 10)
+    at = {name: FIRST + 0x100000 * i for i, name in enumerate(size)}
+    for place in (at[other], at[other] + size[other] - 4 if out != "slots" else at[other] + size[other] - 8, at[other] - size[out] + 8):
+        where = {k: ctypes.c_void_p(v) for k, v in {**at, out: place // 8 * 8 if out == "slots" else place}.items()}
+        if where[out].value + size[out] <= at[other] or where[out].value >= at[other] + size[other]:
+            continue
+        st = binding.library().dps_extend_block_tables(where["lengths"], where["new"], B, where["granted"], G, where["table"], 10, 10, 16, 100, where["after"],
+                                                       where["starts"], where["positions"], where["slots"], T, where["used"], None)
+        assert st == binding.DPS_ERR_DATA, (out, other, place - at[other])
