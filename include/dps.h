@@ -294,7 +294,7 @@ DPS_API dps_status dps_extend_block_tables(const int32_t* lengths, const int32_t
  *   float [max_position][rotated]: rotated/2 cosines, then as many sines.  Pair i is (i, i + rotated/2), or, with
  *   interleaved != 0, (2i, 2i + 1).  rotated: a multiple of 16 up to head_dim; 0: no rotation (positions, cos_sin unused).
  * in 32 bits with one rounding at the end.  Queries go to q_out [T][q_heads][head_dim] (row stride q_out_stride; it may
- * be qkv itself, with qkv's stride), keys and values (unchanged) to slots[t] of the cache.  A row with a negative slot is padding: nothing is
+ * be qkv itself, with qkv's stride, or columns beside qkv's in one buffer; any other overlap is refused with DPS_ERR_DATA), keys and values (unchanged) to slots[t] of the cache.  A row with a negative slot is padding: nothing is
  * written for it.  A row whose slot or position is out of range is skipped and flagged.  The slots of a call must
  * differ.  A cache of page_tokens = 1 and slots 0, 1, .. makes plain rows of keys and values.
  */

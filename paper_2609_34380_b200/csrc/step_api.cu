@@ -96,8 +96,17 @@ dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t T, int3
     if ((q_weight == nullptr) != (k_weight == nullptr)) return DPS_ERR_NULL;
     if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cos_sin, 16) || !aligned(q_weight, 16) || !aligned(k_weight, 16)) return DPS_ERR_ALIGN;
     if (!aligned(slots, 8) || !aligned(positions, 4)) return DPS_ERR_ALIGN;
-    // in place each warp writes what it has read itself; with other strides it would write another one's
-    if (q_out == qkv && q_heads > 0 && T > 1 && q_out_stride != qkv_stride) return DPS_ERR_DATA;
+    // in place each warp writes what it has read itself; with other strides, or over other columns, it would write another one's.  (Rows of one stride may
+    // lie between each other: columns of one wide buffer.)
+    if (q_heads > 0 && (q_out != qkv || (T > 1 && q_out_stride != qkv_stride))) {
+        const auto span = [&](int64_t stride, int64_t width) { return (size_t)(((T - 1) * (T > 1 ? stride : 0) + width) * 2); };
+        if (overlap(qkv, span(qkv_stride, row), q_out, span(q_out_stride, q_row))) {
+            if (T == 1 || q_out_stride != qkv_stride) return DPS_ERR_DATA;
+            const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(q_out) - reinterpret_cast<uintptr_t>(qkv)) / 2 % qkv_stride;
+            const int64_t column = apart < 0 ? apart + qkv_stride : apart;      // of the queries in qkv's rows
+            if (column < row || column + q_row > qkv_stride) return DPS_ERR_DATA;
+        }
+    }
     int* status;
     const dps_status st = device_status_word(&status);
     if (st != DPS_OK) return st;

@@ -22,3 +22,21 @@ def test_extend_block_tables(out, other):
         st = binding.library().dps_extend_block_tables(where["lengths"], where["new"], B, where["granted"], G, where["table"], 10, 10, 16, 100, where["after"],
                                                        where["starts"], where["positions"], where["slots"], T, where["used"], None)
         assert st == binding.DPS_ERR_DATA, (out, other, place - at[other])
+
+
+@pytest.mark.parametrize("column", [8, 64, 512, 576, 768 - 8, -8, -504, 2 * 768 + 8])
+@pytest.mark.parametrize("T", [1, 3])
+def test_queries_over_other_columns(T, column):
+    """Eight query heads and two of keys and values, 64 elements each: queries written over anything but themselves."""
+    if T == 1 and column > 768:
+        return
+    c = binding.KvCache(k=0x10000, v=0x20000, blocks=10, block_stride=16 * 2 * 64, token_stride=2 * 64, head_stride=64, page_tokens=16, heads=2, head_dim=64, type=0)
+    fake = [ctypes.c_void_p(0x40000 * (i + 1)) for i in range(3)]
+
+    def call(stride, out_stride, at=column):
+        return binding.library().dps_qk_norm_rope(ctypes.c_void_p(FIRST), stride, T, 8, ctypes.byref(c), fake[0], fake[1], fake[2], 100, 64, 0, None, None, 1e-6,
+                                                  ctypes.c_void_p(FIRST + 2 * at), out_stride, None)
+    assert call(768, 768) == binding.DPS_ERR_DATA
+    assert call(768, 512) == binding.DPS_ERR_DATA
+    if T > 1:                                               # rows with room between them, too little for the queries
+        assert call(1272, 1272, 768) == binding.DPS_ERR_DATA and call(1272, 1272, 768 - 1272) == binding.DPS_ERR_DATA
