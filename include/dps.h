@@ -307,7 +307,8 @@ DPS_API dps_status dps_qk_norm_rope(const void* qkv, int64_t qkv_stride, int64_t
  * Attention of one new token per request over the paged cache:
  *   out[b][h][:] = sum_t p_t V[t][h / (q_heads / heads)][:],  p = softmax_t(scale * q[b][h] . K[t][h / (q_heads / heads)]),
  * t over the lengths[b] tokens that row b of block_table names (block_table[b][t / page_tokens]).  q: [B] rows of q_heads heads
- * (strides q_row_stride, q_head_stride, multiples of 8 elements); out: contiguous [B][q_heads][head_dim].  q_heads is
+ * (strides q_row_stride, q_head_stride, multiples of 8 elements); out: contiguous [B][q_heads][head_dim], which may be q itself if that is so too, and is
+ * refused (DPS_ERR_DATA) over q in any other way.  q_heads is
  * a multiple of cache->heads; B * q_heads * (table_width * page_tokens / 64 + 2) is below 2^38.  Scores, maxima and sums in 32 bits, one rounding at the end; the
  * weights p_t meet the values as sums of two 16-bit numbers, which hold 16 bits of a weight with a BF16 cache, 22 with an FP16 one, there nothing
  * finer than 2^-39 of the largest weight.  An infinite element of V makes its element of the output that infinity, whatever the token's weight; NaN if

@@ -15,6 +15,14 @@ inline bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes
     return x < y + b_bytes && y < x + a_bytes;
 }
 
+// Whether `bytes` bytes at `out` lie over one of n rows of `width` bytes, `stride` apart.  (Room between the rows is no row, if they follow one another.)
+bool over_rows(const void* out, size_t bytes, const void* rows, int64_t n, int64_t stride, int64_t width) {
+    if (bytes == 0 || n == 0 || width <= 0 || !overlap(out, bytes, rows, (size_t)((n > 1 ? (n - 1) * stride : 0) + width))) return false;
+    if (n == 1 || stride < width) return true;
+    const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(rows)) % stride, column = apart < 0 ? apart + stride : apart;
+    return column < width || column + (int64_t)bytes > stride;
+}
+
 dps_status check_cache(const dps_kv_cache* c) {
     if (c == nullptr) return DPS_ERR_NULL;
     if (c->type != DPS_TYPE_FP16 && c->type != DPS_TYPE_BF16) return DPS_ERR_UNSUPPORTED;
@@ -135,6 +143,10 @@ dps_status dps_paged_attention(const void* q, int64_t q_row_stride, int64_t q_he
     if (!aligned(q, 16) || !aligned(out, 16) || !aligned(block_table, 4) || !aligned(lengths, 4)) return DPS_ERR_ALIGN;
     if (!workspace || !aligned(workspace, 16)) return DPS_ERR_WORKSPACE;
     if (workspace_bytes < attention_workspace_bytes(q_heads, cache->heads, cache->head_dim)) return DPS_ERR_WORKSPACE;
+    // in place the queries that a result replaces are its own, which all its parts have read; in another layout they would be others'
+    const int64_t dense = (int64_t)q_heads * cache->head_dim;
+    const bool in_place = out == q && (B == 1 || q_row_stride == dense) && (q_heads == 1 || q_head_stride == cache->head_dim);
+    if (!in_place && over_rows(out, (size_t)(B * dense * 2), q, B, q_row_stride * 2, ((q_heads - 1) * q_head_stride + cache->head_dim) * 2)) return DPS_ERR_DATA;
     int* status;
     const dps_status st = device_status_word(&status);
     if (st != DPS_OK) return st;

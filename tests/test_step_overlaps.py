@@ -40,3 +40,14 @@ def test_queries_over_other_columns(T, column):
     assert call(768, 512) == binding.DPS_ERR_DATA
     if T > 1:                                               # rows with room between them, too little for the queries
         assert call(1272, 1272, 768) == binding.DPS_ERR_DATA and call(1272, 1272, 768 - 1272) == binding.DPS_ERR_DATA
+
+
+@pytest.mark.parametrize("B,row,head,at", [(3, 512, 64, 64), (3, 512, 64, -8), (3, 512, 64, 1528), (3, 768, 64, 0), (1, 512, 128, 0), (3, 64, 192, 0), (3, 768, 64, 512),
+                                           (3, 4096, 64, 504), (3, 4096, 64, 2568), (3, 4096, 64, 4096 - 1528)])
+def test_results_over_queries(B, row, head, at):
+    """Eight heads of 64 elements: results over queries, unless they are dense and the same."""
+    lib = binding.library()
+    c = binding.KvCache(k=0x10000, v=0x20000, blocks=10, block_stride=16 * 2 * 64, token_stride=2 * 64, head_stride=64, page_tokens=16, heads=2, head_dim=64, type=0)
+    fake = ctypes.c_void_p(0x40000)
+    assert lib.dps_paged_attention(ctypes.c_void_p(FIRST), row, head, B, 8, ctypes.byref(c), fake, 20, 20, fake, 0.1, ctypes.c_void_p(FIRST + 2 * at), fake,
+                                   lib.dps_paged_attention_workspace_bytes(8, 2, 64), None) == binding.DPS_ERR_DATA
