@@ -341,6 +341,7 @@ DPS_API dps_status dps_paged_attention_workspace_init(void* workspace, size_t wo
  * of the largest may be equal though their logits are not.  The weights are formed in 32 bits.  Groups are fast if each is a power of two of lanes at
  * ceil(E / 32) experts a lane: 256, 160, 128 or 64 experts in 8 groups are, 72, 80 or 120 in 8 and 100 in 10 are not (every row is then done in 64 bits).
  * Row t * top_k + j of the outputs is choice j of token t: expert_of_row int32, weights float, token_of_row int32 (may be NULL: it is t).
+ * Outputs over the logits or the bias are refused (DPS_ERR_DATA).
  * A row with a NaN score or choice (a NaN logit; for softmax +Inf, or all -Inf) gets experts -1 and weights 0, and the status word is set.
  * E up to 1024, top_k up to 32 and at most top_groups * (E / groups); groups up to 32.  groups == 1 and top_groups == 1: no groups.
  */

@@ -181,6 +181,12 @@ dps_status dps_route_experts(const void* logits, int64_t logits_stride, int32_t 
     if (!aligned(logits, type == DPS_TYPE_FP32 ? 4 : 2) || !aligned(bias, 4) || !aligned(token_of_row, 4) || !aligned(expert_of_row, 4) ||
         !aligned(weights, 4))
         return DPS_ERR_ALIGN;
+    // a warp writes its token's choices while others have yet to read their logits
+    const int64_t size = type == DPS_TYPE_FP32 ? 4 : 2;
+    const size_t choices = (size_t)(T * top_k) * 4;
+    for (const void* out : {(const void*)token_of_row, (const void*)expert_of_row, (const void*)weights})
+        if (out != nullptr && (over_rows(out, choices, logits, T, logits_stride * size, E * size) || (bias != nullptr && overlap(out, choices, bias, (size_t)E * 4))))
+            return DPS_ERR_DATA;
     int* status;
     const dps_status st = device_status_word(&status);
     if (st != DPS_OK) return st;

@@ -51,3 +51,14 @@ def test_results_over_queries(B, row, head, at):
     fake = ctypes.c_void_p(0x40000)
     assert lib.dps_paged_attention(ctypes.c_void_p(FIRST), row, head, B, 8, ctypes.byref(c), fake, 20, 20, fake, 0.1, ctypes.c_void_p(FIRST + 2 * at), fake,
                                    lib.dps_paged_attention_workspace_bytes(8, 2, 64), None) == binding.DPS_ERR_DATA
+
+
+@pytest.mark.parametrize("out", ["token", "expert", "weights"])
+@pytest.mark.parametrize("type_,stride,at", [(0, 64, 0), (0, 64, 4 * 64 * 2 - 4), (0, 64, -60), (2, 64, 1000), (1, 200, 120), (1, 200, 340), (0, 64, "bias"), (2, 200, "bias")])
+def test_choices_over_logits(out, type_, stride, at):
+    """Four tokens of 64 experts, four choices each (64 bytes): outputs over the logits, by their first or last bytes too, or over the bias."""
+    far = {"logits": FIRST, "bias": FIRST + 0x100000, "token": FIRST + 0x200000, "expert": FIRST + 0x300000, "weights": FIRST + 0x400000}
+    far[out] = far["bias"] + 252 if at == "bias" else FIRST + at
+    p = {k: ctypes.c_void_p(v) for k, v in far.items()}
+    assert binding.library().dps_route_experts(p["logits"], stride, type_, 4, 64, p["bias"], 0, 1, 1, 4, 1, 1.0, p["token"], p["expert"], p["weights"],
+                                               None) == binding.DPS_ERR_DATA
